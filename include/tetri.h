@@ -434,6 +434,94 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
                                                     int32_t append, void *out, void *stream);
 
 /*
+ * Eviction from the paged cache by accumulated attention weight (an extension of this build, not of the paper: Sec. 3.4 names the
+ * decode instance's memory as what limits its batch; here a request gives back the slots of tokens that nobody looks at).
+ * The state is one float per slot, for the caller to keep beside kv_pages and to use with the same block tables:
+ *     kv_weights [num_pages][num_kv_heads][page_size] float: the softmax weight the token in that slot has received so far, from
+ *                all the query heads that share the kv head; 16-byte aligned
+ * Slots that hold no token yet need no value.  The calls:
+ *   tetri_chunk_prefill_weights  adds what rows of a prefill chunk give          \ either or both, in any order with the calls
+ *   tetri_decode_attn_weights    a decode iteration that adds what it gives      / that append
+ *   tetri_kv_select              which slots of every request and kv head stay
+ *   tetri_kv_compact             moves what stays to the front of the cache; ctx_lens shrinks, pages behind it are free again
+ * The kv heads of a request keep the same number of tokens, not the same tokens.  Attention does not depend on the order of the
+ * cache, so afterwards every call works as before on the shorter cache; position information is in K itself and stays.
+ * Scores, exponentials, sums and weights are fp32.  Results are deterministic run to run.  The calls use the caller's workspace
+ * where they need any (16-byte aligned device memory, contents of no meaning before and after): calls that may overlap in time,
+ * and graphs whose replays may, need one each.
+ */
+
+/*
+ * Adds to kv_weights what the last rows of every segment of a chunk give to the keys they see.  With n_s rows of segment s and
+ * t running over its last min(n_s, last_rows) rows, for every kv head and slot j of the request
+ *     w_j = sum over t >= j - ctx_lens[s], query heads h of the kv head:  softmax_j(scale * q[cu[s]+t][h] . K_s[0 .. ctx_lens[s]+t])
+ *     j <  ctx_lens[s]:                    kv_weights at slot j += w_j
+ *     ctx_lens[s] <= j < ctx_lens[s]+n_s:  kv_weights at slot j  = w_j    (the chunk's own tokens; whether or not tetri_kv_append
+ *                                          has run), also where w_j = 0
+ * K_s as for tetri_chunk_prefill_attn: kv_pages for j < ctx_lens[s], k_new otherwise.  last_rows >= chunk_size counts every row.
+ *   q [chunk_size][num_q_heads][head_dim], k_new [chunk_size][num_kv_heads][head_dim], kv_pages, block_table, cu_chunk_q_lens,
+ *   ctx_lens: device, in.  kv_weights: device, in/out.  fp8: 1 = kv_pages is a pool of E4M3 codes under k_scale (otherwise
+ *   ignored); k_new is bf16 either way.  num_segs: 1..max_segs_per_chunk.  last_rows >= 1.
+ *   max_ctx_len: host scalar, an upper bound of ctx_lens; a segment whose context is longer is left out.
+ *   workspace: at least tetri_chunk_prefill_weights_workspace(num_segs, max_ctx_len, last_rows) bytes (a negative tetri_status for
+ *   arguments that the call would refuse).
+ * Errors as for tetri_chunk_prefill_attn; TETRI_ERR_INVALID_ARG also for a workspace that is too small.
+ */
+TETRI_API int64_t tetri_chunk_prefill_weights_workspace(tetri_ctx *ctx, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows);
+TETRI_API tetri_status tetri_chunk_prefill_weights(tetri_ctx *ctx, const void *q, const void *k_new, const void *kv_pages, float *kv_weights,
+                                                   const int32_t *block_table, const int32_t *cu_chunk_q_lens, const int32_t *ctx_lens,
+                                                   int32_t num_segs, int32_t max_ctx_len, int32_t last_rows, float scale, int32_t fp8,
+                                                   float k_scale, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * A decode iteration that also adds its softmax weights: `out` and, with append = 1, the pool are those of tetri_decode_attn /
+ * tetri_decode_attn_append (fp8 = 1: tetri_decode_attn_fp8 under k_scale and v_scale), and for every request b, kv head and slot
+ * j < ctx_lens[b] the weight that the new token's query heads give to K_b[j] is added to kv_weights; with append = 1 what they give to
+ * the new token itself becomes the weight of its slot, ctx_lens[b].
+ *   max_ctx_len is an upper bound of ctx_lens here in earnest: of a request that is longer no weight is added.
+ *   workspace: at least tetri_decode_attn_weights_workspace(num_reqs, max_ctx_len) bytes (a negative tetri_status for arguments that
+ *   the call would refuse).
+ * Other arguments, errors and the scratch-memory rule as for those calls.
+ */
+TETRI_API int64_t tetri_decode_attn_weights_workspace(tetri_ctx *ctx, int32_t num_reqs, int32_t max_ctx_len);
+TETRI_API tetri_status tetri_decode_attn_weights(tetri_ctx *ctx, const void *q, const void *k_new, const void *v_new, void *kv_pages,
+                                                 float *kv_weights, const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs,
+                                                 int32_t max_ctx_len, float scale, int32_t append, int32_t fp8, float k_scale, float v_scale,
+                                                 void *workspace, int64_t workspace_bytes, void *out, void *stream);
+
+/*
+ * Which slots of every request and kv head stay when its cache is cut to `keep` tokens.  With L = ctx_lens[b], n = min(L, keep) and
+ * r = min(recent, n): the last r slots [L - r, L), and of the slots in front of them the n - r with the largest weight, among equal
+ * ones the lowest slot first (a NaN counts as -infinity).  The answer says where the token of every new slot is now:
+ *     slots [num_reqs][num_kv_heads][keep] int32
+ *       L <= keep:              slots[i] = i for i < L
+ *       otherwise  i <  n - r:  i itself where slot i stays; the k-th i that does not gets the k-th staying slot of [n - r, L - r)
+ *                  i >= n - r:  i + L - n
+ *       i >= n:                 -1
+ *     new_lens [num_reqs] int32: n, the ctx_lens after tetri_kv_compact (another array than ctx_lens)
+ * So as few tokens move as can, and the last r slots are the newest r tokens, oldest first, again.
+ *   kv_weights, block_table [num_reqs][max_blocks_per_seq], ctx_lens: device, in.  slots (16-byte aligned), new_lens: device, out.
+ *   max_ctx_len: an upper bound of ctx_lens; of a longer request only the first max_ctx_len slots count.  1 <= keep <=
+ *   max_blocks_per_seq * page_size, 0 <= recent <= keep.
+ * TETRI_ERR_UNSUPPORTED for max_ctx_len above 524288.
+ */
+TETRI_API tetri_status tetri_kv_select(tetri_ctx *ctx, const float *kv_weights, const int32_t *block_table, const int32_t *ctx_lens,
+                                       int32_t num_reqs, int32_t max_ctx_len, int32_t keep, int32_t recent, int32_t *slots,
+                                       int32_t *new_lens, void *stream);
+
+/*
+ * Moves the tokens that stay, in place: afterwards slot i < n of request b and a kv head holds what slot slots[b][head][i] held, K, V
+ * and weight; slots at and behind n hold nothing of meaning (those at and behind the old ctx_lens[b] are not touched).
+ *   slots, block_table, ctx_lens (as it was for tetri_kv_select, not new_lens), num_reqs, keep, recent: as for tetri_kv_select, whose
+ *   map it has to be (of another one no more is promised than that no slot but the requests' own is read or written).
+ *   kv_pages, kv_weights: device, in/out.  fp8: 1 = kv_pages is a pool of E4M3 codes.
+ * The requests' pages must be distinct.
+ */
+TETRI_API tetri_status tetri_kv_compact(tetri_ctx *ctx, const int32_t *slots, const int32_t *block_table, const int32_t *ctx_lens,
+                                        int32_t num_reqs, int32_t keep, int32_t recent, void *kv_pages, float *kv_weights, int32_t fp8,
+                                        void *stream);
+
+/*
  * Debug check of device-resident chunk metadata.  Synchronises `stream`, copies the arrays to
  * the host and checks: cu[0] == 0, cu strictly increasing, cu[num_segs] <= chunk_size,
  * ctx_lens >= 0, every needed block-table entry in [0, num_pages), enough logical pages

@@ -9,7 +9,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetri.so")
 NATIVE = os.path.join(HERE, "_native.so")
-SOURCES = ["tetri_host.cpp", "tetri_plan.cpp", "tetri_append.hip", "tetri_kv_transfer.hip", "tetri_decode.hip", "tetri_attn.hip", "tetri_planned.hip", "tetri_short.hip"]
+SOURCES = ["tetri_host.cpp", "tetri_evict_host.cpp", "tetri_plan.cpp", "tetri_append.hip", "tetri_kv_transfer.hip", "tetri_decode.hip", "tetri_attn.hip", "tetri_planned.hip", "tetri_short.hip",
+           "tetri_weights.hip", "tetri_evict.hip"]
 HEADERS = [os.path.join(CSRC, "tetri_internal.h"), os.path.join(CSRC, "tetri_plan.h"), os.path.join(CSRC, "attn_common.h"), os.path.join(CSRC, "attn_tile.h"), os.path.join(ROOT, "include", "tetri.h")]
 
 # packed-fp32 instructions are switched off for all device code; a kernel's leading scalar arguments (up to 14 words in front of

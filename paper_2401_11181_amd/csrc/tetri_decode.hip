@@ -37,6 +37,7 @@
 // the new token, which is not quantised, is a step of its own (one key in a matrix product) with its weight divided by the
 // V scale.
 #include <mutex>
+#include <type_traits>
 
 #include "attn_common.h"
 
@@ -46,8 +47,9 @@ using namespace tetri_dev;
 
 constexpr int kMergeCols = 4;     // query heads whose partial O the merge area in LDS holds at a time
 
-// A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
-template <int D> __device__ __forceinline__ int part_floats(int g) { return g * D + ((2 * g + 3) & ~3); }
+// A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum; W: and g of the sum of the
+// weights before they were rounded.
+template <int D, bool W> __device__ __forceinline__ int part_floats(int g) { return g * D + (((W ? 3 : 2) * g + 3) & ~3); }
 
 __device__ __forceinline__ float load_coherent(const float *p)
 {
@@ -107,7 +109,7 @@ __device__ __forceinline__ void issue_last(const char *page_lo, const char *page
     }
 }
 
-typedef __attribute__((address_space(4))) const DecodeArgs const_decode_args;
+template <bool W> using DecodeKernelArgs = std::conditional_t<W, DecodeWeightArgs, DecodeArgs>;
 
 // A stretch of steps of one request; wave-uniform.
 struct Job {
@@ -125,16 +127,19 @@ static_assert((kDecodeLead + offsetof(DecodeArgs, k_new)) % 64 == 0 && offsetof(
 
 // RANGES: `ranges` equal ranges of the batch's steps, a workgroup each per kv head; otherwise every (request, kv head) in
 // `parts` equal parts, a workgroup each.  Grid: kv head fastest.
-template <int D, bool FP8, int NW, bool RANGES>
+// W: the scores and the softmax's sum go to memory too (see tetri_weights.hip for what becomes of them).  The sum is another one
+// than the output is divided by: that one is of the weights as rounded for the PV product.
+template <int D, bool FP8, int NW, bool RANGES, bool W>
 __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *ctx_lens, const int32_t *bt, const uint16_t *pages, int max_blocks, int Hkv,
-                                                                  uint32_t hkv_magic, int parts, const uint16_t *q, int B, DecodeArgs)
+                                                                  uint32_t hkv_magic, int parts, const uint16_t *q, int B, DecodeKernelArgs<W>)
 {
+    typedef __attribute__((address_space(4))) const DecodeKernelArgs<W> const_decode_args;
     typedef Tile<D, FP8> T;
     constexpr int KSTEPS = D / 16, DBLK = D / 32, NI = T::NI, NT = NW * 64, ROW = 2 * D;
     constexpr int DEPTH = FP8 ? 2 : 1;                     // steps a wavefront's tiles hold
     __shared__ __attribute__((aligned(1024))) char smem[NW * DEPTH * 2 * T::BYTES];
     __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
-    __shared__ float stat[NW][2][32];
+    __shared__ float stat[NW][W ? 3 : 2][32];
     __shared__ int arrived;
     // (the structure lies behind the leading arguments)
     const const_decode_args *p = (const const_decode_args *)((__attribute__((address_space(4))) const char *)__builtin_amdgcn_kernarg_segment_ptr() + kDecodeLead);
@@ -316,6 +321,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
     for (;;) {                                           // the jobs of the range
     f32x16 o[DBLK];
     float m = -1e30f, lsum = 0.f;                        // m: a reference exponent, not the exact maximum
+    [[maybe_unused]] float lfull = 0.f;                  // W: the sum of the weights before they are rounded
 #pragma unroll
     for (int i = 0; i < DBLK; ++i)
 #pragma unroll
@@ -356,13 +362,36 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             for (int v = 0; v < 16; ++v)
                 if (key_of(v) > new_row - (FP8 ? 1 : 0)) sc[v] = masked;
         }
+        if constexpr (W) {
+            // four or eight neighbouring keys of a query head to a lane.  (A step past the row's end: a context longer than the caller said)
+            const int stride = p->score_stride;
+            if (cs * 32 < stride && l32 < p->g) {
+                float *row = p->scores + ((size_t)cb * p->Hq + (size_t)kh * p->g + l32) * stride + cs * 32;
+#pragma unroll
+                for (int v = 0; v < 16; v += 4) {
+                    const f32x4 t = {sc[v] * c, sc[v + 1] * c, sc[v + 2] * c, sc[v + 3] * c};
+                    *reinterpret_cast<__attribute__((address_space(1))) f32x4 *>((uintptr_t)(row + key_of(v))) = t;
+                }
+            }
+        }
         bf16x8 pf[2];
+        [[maybe_unused]] float unrounded = 0.f;
         // (a lambda: as a function shared by the kernels it made the short kernel 4 % slower)
         auto weights = [&]() {                           // rounded to bf16 for the PV product
+            if constexpr (W) {
+                unrounded = 0.f;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[v], c, -m));
+                    pf[v / 8][v % 8] = (__bf16)x;
+                    unrounded += x;
+                }
+            } else {
 #pragma unroll
             for (int v = 0; v < 16; v += 2) {
                 pf[v / 8][v % 8] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[v], c, -m));
                 pf[v / 8][v % 8 + 1] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[v + 1], c, -m));
+            }
             }
         };
         if (first) {
@@ -377,6 +406,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                 const float alpha = __builtin_amdgcn_exp2f(m - m_new);
                 m = m_new;
                 lsum *= alpha;
+                if constexpr (W) lfull *= alpha;
 #pragma unroll
                 for (int i = 0; i < DBLK; ++i)
 #pragma unroll
@@ -385,6 +415,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             }
         }
         add_weights(pf, lsum);
+        if constexpr (W) lfull += unrounded;
         // V has landed when only what was issued after it is outstanding
         if constexpr (FP8) {
             if (far) wait_vm<3 * NI>();
@@ -440,6 +471,11 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                 m = m_new;
                 const __bf16 wgt = (__bf16)__builtin_amdgcn_exp2f(score - m);
                 lsum = lsum * alpha + (half == 0 ? (float)wgt : 0.f);
+                if constexpr (W) {
+                    lfull = lfull * alpha + (half == 0 ? __builtin_amdgcn_exp2f(score - m) : 0.f);
+                    if (lane < p->g)
+                        *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(p->new_scores + (size_t)cb * p->Hq + (size_t)kh * p->g + lane)) = score;
+                }
                 bf16x8 pn = __builtin_bit_cast(bf16x8, none);
                 if (half == 0) pn[0] = (__bf16)((float)wgt * p->v_inv);
 #pragma unroll
@@ -475,6 +511,10 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
     const bool ends = job.end == job.steps(), whole = ends && job.begin == 0;
     const float ltot = half_swap_sum(lsum);
     if (half_e == 0) { stat[wave][0][col_e] = m; stat[wave][1][col_e] = ltot; }
+    if constexpr (W) {
+        const float ftot = half_swap_sum(lfull);
+        if (half_e == 0) stat[wave][2][col_e] = ftot;
+    }
     if (ends && e->pages_w != nullptr && job.L < max_blocks * kPage && wave == NW - 1 && (te & 63) < ROW / 8) {
         // fused append: the new token's K and V row of this kv head go to slot L % 16 of page block_table[b][L / 16], 16 bytes
         // per lane (nothing in this launch reads that slot: key L comes from k_new / v_new everywhere).  With an FP8
@@ -516,7 +556,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
         }
         counter = counter * Hkv + kh;
     }
-    const int pfl = part_floats<D>(g);
+    const int pfl = part_floats<D, W>(g);
     float *partial = e->partial;
     auto place = [&](int i) -> float * { return partial + ((size_t)(RANGES ? 2 * (w0 + i) + (int)(i == 0) : w0 + i) * Hkv + kh) * pfl; };
     const size_t head = (size_t)job.b * e->Hq + (size_t)kh * g;
@@ -528,6 +568,9 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
         r[0] = (__bf16)(x * inv);
         r[1] = (__bf16)(y * inv);
         *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)(out + at)) = __builtin_bit_cast(uint32_t, r);
+    };
+    auto write_lse = [&](int col, float ref, float sum) {
+        if constexpr (W) *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(e->lse + head + col)) = ref + __builtin_amdgcn_logf(sum);
     };
     for (int c0 = 0; c0 < g; c0 += kMergeCols) {
         if (c0 != 0) lds_barrier();                      // everybody is done with the columns before
@@ -569,6 +612,15 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                     store_coherent(mine + g * D + g + col, l);
                 }
             }
+            if constexpr (W) {
+                if (d == 0) {
+                    float f = 0.f;
+#pragma unroll
+                    for (int i = 0; i < NW; ++i) f = __builtin_fmaf(stat[i][2][col], __builtin_amdgcn_exp2f(stat[i][0][col] - ms), f);
+                    if (whole) write_lse(col, ms, f);
+                    else store_coherent(place(piece) + g * D + 2 * g + col, f);
+                }
+            }
         }
     }
     if (!whole) {
@@ -580,6 +632,28 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             // all the others have been here: the counter goes back to zero, the parts are merged in their order.  With few
             // columns the threads form groups that take every groups-th part, and the groups meet in LDS.
             if (te == 0) store_global(e->counters + counter, 0);
+            if constexpr (W) {
+                if (te < g) {
+                    float ref = -INFINITY, sum = 0.f;
+                    for (int i0 = 0; i0 < pieces; i0 += 8) {
+                        float mi[8], fi[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float *src = place(min(i0 + i, pieces - 1)) + g * D + te;
+                            mi[i] = load_coherent(src);
+                            fi[i] = load_coherent(src + 2 * g);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (i0 + i < pieces) {
+                                const float m_new = fmaxf(ref, mi[i]);
+                                sum = __builtin_fmaf(fi[i], __builtin_amdgcn_exp2f(mi[i] - m_new), sum * __builtin_amdgcn_exp2f(ref - m_new));
+                                ref = m_new;
+                            }
+                    }
+                    write_lse(te, ref, sum);
+                }
+            }
             const int pairs = g * (D / 2), groups = max(1, NT / pairs);
             for (int v0 = 0; v0 < pairs; v0 += NT) {
                 const int grp = groups > 1 ? te / pairs : 0, v = groups > 1 ? te - grp * pairs : v0 + te;
@@ -670,20 +744,24 @@ hipError_t tetri_decode_static_memory(DecodeStatic *out)
     return hipSuccess;
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool W>
 static hipError_t launch_decode(const DecodeParams &p, hipStream_t stream)
 {
     const dim3 grid((p.parts > 0 ? p.B * p.parts : p.ranges) * p.Hkv);
-    auto kernel = p.parts > 0 ? decode_attn_kernel<D, FP8, 4, false> : decode_attn_kernel<D, FP8, 4, true>;
+    auto kernel = p.parts > 0 ? decode_attn_kernel<D, FP8, 4, false, W> : decode_attn_kernel<D, FP8, 4, true, W>;
     static_assert(KernelArgs<decltype(kernel)>::last_offset() == kDecodeLead, "where the kernel reads its structure");
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p.ctx, p.bt, p.pages, p.max_blocks, p.Hkv, p.hkv_magic, p.parts, p.q, p.B, static_cast<const DecodeArgs &>(p));
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, p.ctx, p.bt, p.pages, p.max_blocks, p.Hkv, p.hkv_magic, p.parts, p.q, p.B, static_cast<const DecodeKernelArgs<W> &>(p));
     return hipGetLastError();
 }
 
 hipError_t tetri_launch_decode(const tetri_ctx *h, const DecodeParams &p, hipStream_t stream)
 {
     const int d = h->cfg.head_dim;
-    if (d == 128) return p.fp8 ? launch_decode<128, true>(p, stream) : launch_decode<128, false>(p, stream);
-    if (d == 64) return p.fp8 ? launch_decode<64, true>(p, stream) : launch_decode<64, false>(p, stream);
+    if (p.weights) {
+        if (d == 128) return p.fp8 ? launch_decode<128, true, true>(p, stream) : launch_decode<128, false, true>(p, stream);
+        if (d == 64) return p.fp8 ? launch_decode<64, true, true>(p, stream) : launch_decode<64, false, true>(p, stream);
+    }
+    if (d == 128) return p.fp8 ? launch_decode<128, true, false>(p, stream) : launch_decode<128, false, false>(p, stream);
+    if (d == 64) return p.fp8 ? launch_decode<64, true, false>(p, stream) : launch_decode<64, false, false>(p, stream);
     return hipErrorInvalidValue;
 }

@@ -1,0 +1,308 @@
+// Eviction from the paged cache for gfx950: which slots of a request a kv head keeps, and the moves that bring them to the front of
+// the cache.  A request with L cached tokens and n = min(L, keep) to be kept gives up e = L - n of them.  The last r = min(recent, n)
+// slots always stay; of the slots in front of them, [0, L - r), the n - r with the largest weight do, the lowest slot first among
+// equals.  Then
+//   * a kept slot below n - r stays where it is;
+//   * the k-th slot below n - r that is not kept (a hole) takes the k-th kept slot of [n - r, L - r): there are as many of each;
+//   * slot n - r + i takes slot L - r + i: the newest tokens close up, in their order.
+// So as few tokens move as can (attention does not care for the order of the others), and the last slots are the newest tokens again,
+// which is all that the next eviction needs to know.
+#include "attn_common.h"
+
+namespace {
+
+using namespace tetri_dev;
+
+constexpr int kSelectThreads = 1024, kDigits = 2048;
+
+// Sum over the threads in front of this one; `total`: of all.
+__device__ inline int block_scan(int x, int *wave_sums, int &total)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int incl = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(incl, d);
+        if (lane >= d) incl += up;
+    }
+    __syncthreads();                                     // (everybody is done with an earlier scan's sums)
+    if (lane == 63) wave_sums[wave] = incl;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int i = 0; i < kSelectThreads / 64; ++i) {
+        if (i < wave) before += wave_sums[i];
+        total += wave_sums[i];
+    }
+    return before + incl - x;
+}
+
+// A weight as an integer in the same order: NaN below all others with -infinity, -0 as 0.
+__device__ __forceinline__ uint32_t ordered(float w)
+{
+    if (w != w) w = -INFINITY;
+    const uint32_t b = __builtin_bit_cast(uint32_t, w + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+
+// A workgroup per (request, kv head).  The smallest kept weight is found digit by digit (11, 11 and 10 bits, from the top), each by a
+// histogram of the weights that agree with the digits so far; then every slot's bit is known, and the map follows from the counts
+// of bits in front of each word.
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
+{
+    extern __shared__ uint32_t smem[];
+    __shared__ int wave_sums[kSelectThreads / 64];
+    __shared__ int found[3];
+    const int words = (p.max_ctx + 31) / 32;
+    uint32_t *hist = smem, *kept = hist + kDigits, *other = kept + words;    // other: equals, later counts
+    const int tid = threadIdx.x, b = blockIdx.x / p.Hkv, kh = blockIdx.x - b * p.Hkv;
+    const int L = min(min(max(p.ctx[b], 0), p.max_blocks * kPage), p.max_ctx);
+    const int n = min(L, p.keep), r = min(p.recent, n), heavy = n - r, old = L - r;
+    int32_t *to = p.slots + ((size_t)b * p.Hkv + kh) * p.keep;
+    if (kh == 0 && tid == 0) p.new_lens[b] = n;
+    if (L <= p.keep || heavy == 0) {
+        for (int i = tid; i < p.keep; i += kSelectThreads) to[i] = i < n ? i + (L - n) : -1;
+        return;
+    }
+    const int32_t *row = p.bt + (size_t)b * p.max_blocks;
+    auto load4 = [&](int j) -> f32x4 {
+        const size_t at = ((size_t)row[j / kPage] * p.Hkv + kh) * kPage + j % kPage;
+        return *reinterpret_cast<__attribute__((address_space(1))) const f32x4 *>((uintptr_t)(p.weights + at));
+    };
+    uint32_t prefix = 0;
+    int want = heavy;                                    // so many of those that agree with the prefix
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+        const uint32_t mask = pass == 2 ? 1023 : 2047;
+        for (int i = tid; i < kDigits; i += kSelectThreads) hist[i] = 0;
+        __syncthreads();
+        for (int j = 4 * tid; j < old; j += 4 * kSelectThreads) {
+            const f32x4 w = load4(j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t u = ordered(w[i]);
+                if (j + i < old && (pass == 0 || (u >> above) == (prefix >> above))) atomicAdd(&hist[(u >> shift) & mask], 1u);
+            }
+        }
+        __syncthreads();
+        // from the largest digit down: thread i has digits 2047 - 2i and 2046 - 2i
+        const int hi = hist[kDigits - 1 - 2 * tid], lo = hist[kDigits - 2 - 2 * tid];
+        int total;
+        const int before = block_scan(hi + lo, wave_sums, total);
+        if (before < want && before + hi + lo >= want) {
+            const bool first = before + hi >= want;
+            found[0] = kDigits - 1 - 2 * tid - (first ? 0 : 1);
+            found[1] = want - before - (first ? 0 : hi);
+            found[2] = first ? hi : lo;
+        }
+        __syncthreads();
+        prefix |= (uint32_t)found[0] << shift;
+        want = found[1];
+    }
+    const bool all_equals = want == found[2];            // of the weights equal to the smallest kept one, `want` are kept
+    // a bit for every old slot: kept, or equal to the smallest kept weight
+    for (int base = 0; base < words * 32; base += 4 * kSelectThreads) {
+        const int j = base + 4 * tid;
+        uint32_t more = 0, equal = 0;
+        if (j < old) {
+            const f32x4 w = load4(j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t u = ordered(w[i]);
+                if (j + i < old) {
+                    more |= (uint32_t)(u > prefix || (all_equals && u == prefix)) << i;
+                    equal |= (uint32_t)(u == prefix) << i;
+                }
+            }
+        }
+        more <<= 4 * (tid & 7);
+        equal <<= 4 * (tid & 7);
+#pragma unroll
+        for (int d = 1; d < 8; d <<= 1) {
+            more |= __shfl_xor(more, d);
+            equal |= __shfl_xor(equal, d);
+        }
+        if ((tid & 7) == 0 && j < words * 32) {
+            kept[j / 32] = more;
+            other[j / 32] = equal;
+        }
+    }
+    __syncthreads();
+    const int each = (words + kSelectThreads - 1) / kSelectThreads, w0 = min(words, tid * each), w1 = min(words, w0 + each);
+    int total;
+    if (!all_equals) {
+        // the first `want` of the equals
+        int mine = 0;
+        for (int w = w0; w < w1; ++w) mine += __popc(other[w]);
+        int at = block_scan(mine, wave_sums, total);
+        for (int w = w0; w < w1; ++w)
+            for (uint32_t x = other[w]; x != 0 && at < want; x &= x - 1, ++at) kept[w] |= x & -x;
+    }
+    int mine = 0;
+    for (int w = w0; w < w1; ++w) mine += __popc(kept[w]);
+    int at = block_scan(mine, wave_sums, total);
+    for (int w = w0; w < w1; ++w) {
+        other[w] = at;                                   // kept slots in front of the word
+        at += __popc(kept[w]);
+    }
+    __syncthreads();
+    auto kept_before = [&](int j) -> int {               // (j < words * 32)
+        return other[j / 32] + __popc(kept[j / 32] & ((1u << (j % 32)) - 1u));
+    };
+    const int stay = heavy < words * 32 ? kept_before(heavy) : total;
+    for (int i = tid; i < p.keep; i += kSelectThreads) {
+        int src = i < n ? i + (L - n) : -1;
+        if (i < heavy) {
+            src = i;
+            if (!(kept[i / 32] >> (i % 32) & 1)) {
+                const int k = stay + i - kept_before(i);             // its token is kept slot number k
+                int lo = 0, hi = words - 1;                          // the last word with at most k in front of it
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) / 2;
+                    if ((int)other[mid] <= k) lo = mid;
+                    else hi = mid - 1;
+                }
+                uint32_t x = kept[lo];
+                for (int skip = k - (int)other[lo]; skip > 0; --skip) x &= x - 1;
+                src = lo * 32 + __builtin_ctz(x | 0x80000000u);
+            }
+        }
+        to[i] = src;
+    }
+}
+
+// The moves in place.  A token's row of K (or V) of one kv head goes 16 bytes to a lane.  Two kinds:
+//   * to the holes from behind the new end (slots n and up): no other move writes what it reads or reads what it writes, so
+//     all of them may run at once;
+//   * those that have to do with the last r slots [n - r, n): what a hole takes from there, and the newest tokens that come there.  Slot n - r + i
+//     may be read by two moves (by a hole's, and where e < r by that of slot n - r + i - e) before it is written.  One
+//     workgroup goes over these slots in order: it reads a stretch of slots for the holes and the tokens that come into the
+//     stretch, waits until all its reads have returned, and writes.  What it reads later lies behind what it has written.
+constexpr int kCompactThreads = 256, kBack = 1024;
+
+template <int RB>      // bytes of a row
+__global__ __launch_bounds__(kCompactThreads) void compact_kernel(CompactParams p, int tiles)
+{
+    constexpr int LPR = RB / 16, STEP = kCompactThreads / LPR, ROWS = 4, TILE = ROWS * STEP;
+    __shared__ int32_t hole[kBack];
+    const int tid = threadIdx.x, lane_row = tid / LPR, chunk = tid % LPR;
+    int id = blockIdx.x;
+    const int tile = id % (tiles + 1);
+    id /= tiles + 1;
+    const int kv = id % 2;
+    id /= 2;
+    const int kh = id % p.Hkv, b = id / p.Hkv;
+    const int L = min(max(p.ctx[b], 0), p.max_blocks * kPage), n = min(L, p.keep), r = min(p.recent, n), heavy = n - r, e = L - n;
+    if (e == 0) return;
+    const int32_t *map = p.slots + ((size_t)b * p.Hkv + kh) * p.keep, *row = p.bt + (size_t)b * p.max_blocks;
+    auto place = [&](int slot) -> size_t {               // of a slot among all (page, kv head, slot)
+        return ((size_t)row[slot / kPage] * p.Hkv + kh) * kPage + slot % kPage;
+    };
+    auto data = [&](int slot) -> char * {
+        return p.pages + ((((size_t)row[slot / kPage] * 2 + kv) * p.Hkv + kh) * kPage + slot % kPage) * RB + chunk * 16;
+    };
+    auto ld = [&](int slot) -> u32x4 { return *reinterpret_cast<global_u32x4 *>((uintptr_t)data(slot)); };
+    auto st = [&](int slot, u32x4 v) { *reinterpret_cast<global_u32x4_w *>((uintptr_t)data(slot)) = v; };
+    const bool weight = kv == 0 && chunk == 0;           // these lanes move the weights as well
+    if (tile < tiles) {
+        int src[ROWS];
+        u32x4 v[ROWS];
+        float w[ROWS];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int to = tile * TILE + i * STEP + lane_row;
+            src[i] = to < heavy ? map[to] : -1;
+            if (src[i] < n || src[i] >= L) src[i] = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (src[i] >= 0) {
+                v[i] = ld(src[i]);
+                if (weight) w[i] = p.weights[place(src[i])];
+            }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (src[i] >= 0) {
+                const int to = tile * TILE + i * STEP + lane_row;
+                st(to, v[i]);
+                if (weight) p.weights[place(to)] = w[i];
+            }
+        return;
+    }
+    for (int base = 0; base < r; base += kBack) {
+        const int many = min(r - base, kBack);
+        __syncthreads();
+        for (int i = tid; i < many; i += kCompactThreads) hole[i] = -1;
+        __syncthreads();
+        for (int i = tid; i < heavy; i += kCompactThreads) {
+            const int at = map[i] - heavy - base;
+            if (at >= 0 && at < many) hole[at] = i;
+        }
+        __syncthreads();
+        for (int t0 = 0; t0 < many; t0 += TILE) {
+            u32x4 old[ROWS], now[ROWS];
+            float w_old[ROWS], w_now[ROWS];
+            int to[ROWS], at[ROWS];
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const int x = t0 + i * STEP + lane_row;
+                at[i] = x < many ? heavy + base + x : -1;
+                to[i] = x < many ? hole[x] : -1;
+                if (to[i] >= 0) {
+                    old[i] = ld(at[i]);
+                    if (weight) w_old[i] = p.weights[place(at[i])];
+                }
+                if (at[i] >= 0) {
+                    now[i] = ld(at[i] + e);
+                    if (weight) w_now[i] = p.weights[place(at[i] + e)];
+                }
+            }
+            wait_vm<0>();
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                if (to[i] >= 0) {
+                    st(to[i], old[i]);
+                    if (weight) p.weights[place(to[i])] = w_old[i];
+                }
+                if (at[i] >= 0) {
+                    st(at[i], now[i]);
+                    if (weight) p.weights[place(at[i])] = w_now[i];
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+
+static size_t select_lds(int32_t max_ctx) { return ((size_t)kDigits + 2 * ((size_t)(max_ctx + 31) / 32)) * sizeof(uint32_t); }
+
+hipError_t tetri_launch_select(const SelectParams &p, hipStream_t stream)
+{
+    const size_t lds = select_lds(p.max_ctx);
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(select_kernel, dim3((unsigned)(p.B * p.Hkv)), dim3(kSelectThreads), lds, stream, p);
+    return hipGetLastError();
+}
+
+template <int RB> static hipError_t launch_compact(const CompactParams &p, hipStream_t stream)
+{
+    const int rows = 4 * kCompactThreads / (RB / 16), tiles = (p.keep + rows - 1) / rows;
+    const int64_t wgs = (int64_t)p.B * p.Hkv * 2 * (tiles + 1);
+    if (wgs > 0x7fffffff) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((compact_kernel<RB>), dim3((unsigned)wgs), dim3(kCompactThreads), 0, stream, p, tiles);
+    return hipGetLastError();
+}
+
+hipError_t tetri_launch_compact(int row_bytes, const CompactParams &p, hipStream_t stream)
+{
+    if (row_bytes == 256) return launch_compact<256>(p, stream);
+    if (row_bytes == 128) return launch_compact<128>(p, stream);
+    if (row_bytes == 64) return launch_compact<64>(p, stream);
+    return hipErrorInvalidValue;
+}

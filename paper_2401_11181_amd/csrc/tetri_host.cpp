@@ -301,7 +301,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
                                   const void *kv_pages, void *kv_pages_w, const int32_t *block_table,
                                   const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
                                   void *stream, bool fp8 = false, float k_scale = 1.f, float v_scale = 1.f,
-                                  bool static_scratch = false)
+                                  bool static_scratch = false, const DecodeWeights *weights = nullptr)
 {
     if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
     const void *ptrs[] = {q, k_new, v_new, kv_pages, out};
@@ -360,7 +360,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     //    steps (the ranges' look-up and their cuts through short requests cost more than they balance: 10 us against 14 for
     //    48 requests of up to 1180 tokens, 8/2 heads).
     // All as far as the scratch memory (a partial result per part, two per range) and the counters reach.
-    const int64_t part_bytes = (int64_t)4 * (p.g * cfg.head_dim + (2 * p.g + 3) / 4 * 4);
+    const int64_t part_bytes = (int64_t)4 * (p.g * cfg.head_dim + ((weights ? 3 : 2) * p.g + 3) / 4 * 4);
     const int64_t places = room / part_bytes, cus = std::max(h->num_cus, 1);
     p.hkv_magic = p.Hkv <= 1 ? 0u : (uint32_t)((0x100000000ull + p.Hkv - 1) / p.Hkv);
     p.ranges = 0;
@@ -389,6 +389,11 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
                                     : counter_sets(h->counters, p.n_counters, h->counter_turn);
     p.counters = cs.use;
     p.counters_next = cs.clear;
+    p.weights = weights != nullptr;
+    p.scores = weights ? weights->scores : nullptr;
+    p.new_scores = weights ? weights->new_scores : nullptr;
+    p.lse = weights ? weights->lse : nullptr;
+    p.score_stride = weights ? weights->score_stride : 0;
     hipError_t e = tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares && !static_scratch) ++h->counter_turn;
@@ -1409,3 +1414,22 @@ tetri_status tetri_validate_chunk(tetri_ctx *h, const int32_t *block_table, cons
 }
 
 }  // extern "C"
+
+// ---- what the entry points of tetri_evict_host.cpp share with those above
+tetri_status tetri_fail(tetri_ctx *h, tetri_status st, const char *fmt, ...)
+{
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    return fail(h, st, "%s", buf);
+}
+
+tetri_status tetri_decode_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages, void *kv_pages_w,
+                               const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
+                               void *stream, bool fp8, float k_scale, float v_scale, const DecodeWeights *weights)
+{
+    return decode_common(fn, h, q, k_new, v_new, kv_pages, kv_pages_w, block_table, ctx_lens, num_reqs, max_ctx_len, scale, out, stream, fp8, k_scale,
+                         v_scale, false, weights);
+}

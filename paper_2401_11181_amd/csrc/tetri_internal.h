@@ -283,8 +283,16 @@ struct DecodeArgs {
     float v_scale, k_inv;
 };
 
+// The same for an iteration that also gives its softmax weights (tetri_decode_attn_weights).
+struct DecodeWeightArgs : DecodeArgs {
+    float *scores;        // [request][query head][score_stride]: every cached key's score, times scale and log2(e)
+    float *new_scores;    // [request][query head]: the new token's
+    float *lse;           // [request][query head]: log2 of the softmax's sum of exponentials
+    int32_t score_stride; // a multiple of 32
+};
+
 // The launch as the host lays it out: what it adds goes to the kernel as leading scalars, but for the choice of the kernel.
-struct DecodeParams : DecodeArgs {
+struct DecodeParams : DecodeWeightArgs {
     const int32_t *ctx, *bt;
     const uint16_t *pages, *q;
     int32_t max_blocks, Hkv;
@@ -292,6 +300,52 @@ struct DecodeParams : DecodeArgs {
     int32_t parts;        // > 0: each (request, kv head)'s keys in that many equal parts, a workgroup each
     int32_t B;
     int32_t fp8;          // 1: the pool holds E4M3 codes (one byte per element) with per-tensor scales
+    int32_t weights;      // 1: the iteration gives its weights
+};
+
+// What a decode iteration that gives its weights needs besides the arguments of the others (host).
+struct DecodeWeights {
+    float *scores, *new_scores, *lse;
+    int32_t score_stride;
+};
+
+// Adds a decode iteration's weights to those of the slots they fell on (tetri_weights.hip).
+struct AddWeightsParams {
+    const float *scores, *new_scores, *lse;
+    float *weights;       // [page][kv head][slot]
+    const int32_t *bt, *ctx;
+    int32_t B, Hq, Hkv, g, max_blocks, score_stride;
+    int32_t append;       // 1: the new token has a slot
+};
+
+// Weights that the last rows of a chunk's segments give to the keys (tetri_weights.hip).
+struct WeighParams {
+    const uint16_t *q, *k_new, *pages;
+    float *weights;       // [page][kv head][slot]
+    const int32_t *bt, *cu, *ctx;
+    float2 *stats;        // [chunk row][query head][part]: reference exponent and sum of a row's softmax over a part of its keys
+    int32_t S, C, Hq, Hkv, g, max_blocks;
+    int32_t max_ctx;      // longest context
+    int32_t last;         // rows of a segment that are looked at
+    int32_t parts;        // the keys of a row tile in that many parts
+    float c, k_scale;     // scale * log2(e), and the factor of a code's score for a pool of codes
+};
+
+// Which slots of a request are kept (tetri_evict.hip): at most kSelectMost are chosen from, whose bits and their counts fit the LDS.
+constexpr int32_t kSelectMost = 1 << 19;
+struct SelectParams {
+    const float *weights;
+    const int32_t *bt, *ctx;
+    int32_t *slots, *new_lens;
+    int32_t B, Hkv, max_blocks, max_ctx, keep, recent;
+};
+
+// ... and the moves that follow.
+struct CompactParams {
+    const int32_t *slots, *bt, *ctx;
+    char *pages;
+    float *weights;
+    int32_t B, Hkv, max_blocks, keep, recent;
 };
 
 hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, bool fp8_pool, hipStream_t stream);
@@ -304,6 +358,16 @@ hipError_t tetri_launch_decode(const tetri_ctx *h, const DecodeParams &p, hipStr
 // Device addresses (on the current device) of the static memory of tetri_decode_attn_static.
 hipError_t tetri_decode_static_memory(DecodeStatic *out);
 hipError_t tetri_launch_append(const tetri_ctx *h, const AppendParams &p, int32_t chunk_rows, hipStream_t stream);
+hipError_t tetri_launch_add_weights(const AddWeightsParams &p, int32_t max_ctx_len, hipStream_t stream);
+hipError_t tetri_launch_weigh(int head_dim, bool fp8_pool, const WeighParams &p, int num_cus, hipStream_t stream);
+hipError_t tetri_launch_select(const SelectParams &p, hipStream_t stream);
+hipError_t tetri_launch_compact(int row_bytes, const CompactParams &p, hipStream_t stream);
+
+// Parts of the host layer that its files share.
+tetri_status tetri_fail(tetri_ctx *h, tetri_status st, const char *fmt, ...) __attribute__((format(printf, 3, 4)));
+tetri_status tetri_decode_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages, void *kv_pages_w,
+                               const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
+                               void *stream, bool fp8, float k_scale, float v_scale, const DecodeWeights *weights);
 
 // Copies len int32 (rounded up to a multiple of 4) from pinned host memory to the device, both 16-byte aligned; `done` (null:
 // none) is signalled when that has ended.

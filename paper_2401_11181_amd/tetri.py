@@ -91,6 +91,20 @@ def lib():
         L.tetri_kv_export.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_int64, vp, vp]
         L.tetri_kv_import.restype = i32
         L.tetri_kv_import.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_int64, vp, vp]
+        L.tetri_chunk_prefill_weights_workspace.restype = ctypes.c_int64
+        L.tetri_chunk_prefill_weights_workspace.argtypes = [vp, i32, i32, i32]
+        L.tetri_chunk_prefill_weights.restype = i32
+        L.tetri_chunk_prefill_weights.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, f32, i32, f32, vp,
+                                                  ctypes.c_int64, vp]
+        L.tetri_decode_attn_weights_workspace.restype = ctypes.c_int64
+        L.tetri_decode_attn_weights_workspace.argtypes = [vp, i32, i32]
+        L.tetri_decode_attn_weights.restype = i32
+        L.tetri_decode_attn_weights.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, i32, i32, f32, f32, vp,
+                                                ctypes.c_int64, vp, vp]
+        L.tetri_kv_select.restype = i32
+        L.tetri_kv_select.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+        L.tetri_kv_compact.restype = i32
+        L.tetri_kv_compact.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, vp]
         L.tetri_validate_chunk.restype = i32
         L.tetri_validate_chunk.argtypes = [vp, vp, vp, vp, i32, vp]
         L.tetri_batch_create.restype = i32
@@ -342,6 +356,45 @@ class Tetri:
                         stream=None):
         rc = self._n.tetri_kv_import(self._p, buf, block_table, cu_tokens, first_tokens, num_reqs, total_tokens,
                                      kv_pages, stream)
+        if rc:
+            self._check(rc)
+
+    def _size(self, n):
+        if n < 0:
+            raise TetriError(int(n), tetri_last_error(self))
+        return int(n)
+
+    def tetri_chunk_prefill_weights_workspace(self, num_segs, max_ctx_len, last_rows):
+        return self._size(lib().tetri_chunk_prefill_weights_workspace(self.h, int(num_segs), int(max_ctx_len), int(last_rows)))
+
+    def tetri_chunk_prefill_weights(self, q, k_new, kv_pages, kv_weights, block_table, cu_chunk_q_lens, ctx_lens, num_segs,
+                                    max_ctx_len, last_rows, scale, fp8, k_scale, workspace, workspace_bytes, stream=None):
+        rc = self._n.tetri_chunk_prefill_weights(self._p, q, k_new, kv_pages, kv_weights, block_table, cu_chunk_q_lens, ctx_lens,
+                                                 num_segs, max_ctx_len, last_rows, scale, fp8, k_scale, workspace,
+                                                 workspace_bytes, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_decode_attn_weights_workspace(self, num_reqs, max_ctx_len):
+        return self._size(lib().tetri_decode_attn_weights_workspace(self.h, int(num_reqs), int(max_ctx_len)))
+
+    def tetri_decode_attn_weights(self, q, k_new, v_new, kv_pages, kv_weights, block_table, ctx_lens, num_reqs, max_ctx_len, scale,
+                                  append, fp8, k_scale, v_scale, workspace, workspace_bytes, out, stream=None):
+        rc = self._n.tetri_decode_attn_weights(self._p, q, k_new, v_new, kv_pages, kv_weights, block_table, ctx_lens, num_reqs,
+                                               max_ctx_len, scale, append, fp8, k_scale, v_scale, workspace, workspace_bytes,
+                                               out, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_kv_select(self, kv_weights, block_table, ctx_lens, num_reqs, max_ctx_len, keep, recent, slots, new_lens, stream=None):
+        rc = self._n.tetri_kv_select(self._p, kv_weights, block_table, ctx_lens, num_reqs, max_ctx_len, keep, recent, slots,
+                                     new_lens, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_kv_compact(self, slots, block_table, ctx_lens, num_reqs, keep, recent, kv_pages, kv_weights, fp8, stream=None):
+        rc = self._n.tetri_kv_compact(self._p, slots, block_table, ctx_lens, num_reqs, keep, recent, kv_pages, kv_weights, fp8,
+                                      stream)
         if rc:
             self._check(rc)
 
