@@ -65,18 +65,27 @@ int64_t decode_bytes(const tetri_ctx *h, int32_t num_reqs, int32_t max_ctx_len)
     return (int64_t)num_reqs * h->cfg.num_q_heads * (score_stride(max_ctx_len) + 2) * 4;
 }
 
-// In how many parts the keys of a row tile are cut: as many as give every compute unit four workgroups, none of fewer than
-// eight tiles of keys (two to a wavefront).
-int32_t weigh_parts(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
+// How the first pass of weighing a chunk is cut.  Wavefronts of a workgroup that have rows of their own share the keys they read; with as
+// many as a segment's rows fill, on average.  The keys of a row tile are cut in as many parts as give every compute unit two
+// workgroups, none of fewer than eight tiles of keys.
+struct WeighShape {
+    int32_t row_waves, parts;
+};
+WeighShape weigh_shape(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
 {
-    const int64_t g = h->cfg.num_q_heads / h->cfg.num_kv_heads, rows = std::min<int64_t>(h->cfg.chunk_size, (int64_t)num_segs * last_rows);
-    const int64_t wgs = (rows * g + 31) / 32 * h->cfg.num_kv_heads, tiles = ((int64_t)max_ctx_len + std::min(h->cfg.chunk_size, last_rows)) / 32 + 2;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({4 * std::max(h->num_cus, 1) / wgs, tiles / 8, 64}));
+    const int64_t g = h->cfg.num_q_heads / h->cfg.num_kv_heads, rows = std::min<int64_t>(h->cfg.chunk_size, (int64_t)num_segs * last_rows) * g;
+    const int64_t mean = rows / num_segs;
+    WeighShape w;
+    w.row_waves = mean >= 512 ? 4 : mean > 64 ? 2 : 1;
+    const int64_t tile = 64 * w.row_waves, wgs = (rows + tile - 1) / tile * h->cfg.num_kv_heads;
+    const int64_t tiles = ((int64_t)max_ctx_len + std::min(h->cfg.chunk_size, last_rows)) / 32 + 2;
+    w.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * std::max(h->num_cus, 1) / wgs, tiles / 8, 64}));
+    return w;
 }
 
 int64_t weigh_bytes(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
 {
-    return (int64_t)h->cfg.chunk_size * h->cfg.num_q_heads * weigh_parts(h, num_segs, max_ctx_len, last_rows) * 8;
+    return (int64_t)h->cfg.chunk_size * h->cfg.num_q_heads * weigh_shape(h, num_segs, max_ctx_len, last_rows).parts * 8;
 }
 
 }  // namespace
@@ -166,11 +175,15 @@ tetri_status tetri_chunk_prefill_weights(tetri_ctx *h, const void *q, const void
     p.S = num_segs; p.C = c.chunk_size; p.Hq = c.num_q_heads; p.Hkv = c.num_kv_heads; p.g = p.Hq / p.Hkv;
     p.max_blocks = c.max_blocks_per_seq; p.max_ctx = max_ctx_len;
     p.last = std::min(last_rows, c.chunk_size);
-    p.parts = weigh_parts(h, num_segs, max_ctx_len, last_rows);
-    p.c = scale * 1.4426950408889634f;
-    p.k_scale = k_scale;
+    const WeighShape shape = weigh_shape(h, num_segs, max_ctx_len, last_rows);
+    p.row_waves = shape.row_waves; p.parts = shape.parts;
+    p.g_magic = p.g <= 1 ? 0u : (uint32_t)((0x100000000ull + p.g - 1) / p.g);
+    // (never 0: a masked score is an infinity, which the factor turns into -infinity)
+    const auto factor = [&](float of) { return std::copysign(std::fmax(std::fabs(scale) * 1.4426950408889634f * of, 1e-30f), scale); };
+    p.c = factor(1.f);
+    p.c_codes = factor(fp8 ? k_scale : 1.f);
     const int64_t rows = std::min<int64_t>(p.C, (int64_t)p.S * p.last) * p.g;
-    if ((rows / 32 + p.S) * p.parts * p.Hkv > 0x7fffffff || (int64_t)p.C * p.g > 0x7fffffff)
+    if ((rows / 64 + p.S) * p.parts * p.Hkv > 0x7fffffff || ((int64_t)p.C * p.g + 64) * p.g > 0xffffffffll)
         return tetri_fail(h, TETRI_ERR_INVALID_ARG, "%s: too many rows for one launch", fn);
     const hipError_t e = tetri_launch_weigh(c.head_dim, fp8 != 0, p, h->num_cus, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return tetri_fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));

@@ -327,8 +327,10 @@ struct WeighParams {
     int32_t S, C, Hq, Hkv, g, max_blocks;
     int32_t max_ctx;      // longest context
     int32_t last;         // rows of a segment that are looked at
+    int32_t row_waves;    // wavefronts of a workgroup that have different rows (1, 2 or 4)
     int32_t parts;        // the keys of a row tile in that many parts
-    float c, k_scale;     // scale * log2(e), and the factor of a code's score for a pool of codes
+    uint32_t g_magic;     // ceil(2^32 / g), 0 for 1
+    float c, c_codes;     // scale * log2(e), and the same for scores of codes
 };
 
 // Which slots of a request are kept (tetri_evict.hip): at most kSelectMost are chosen from, whose bits and their counts fit the LDS.
