@@ -79,13 +79,14 @@ WeighShape weigh_shape(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len
     w.row_waves = mean >= 512 ? 4 : mean > 64 ? 2 : 1;
     const int64_t tile = 64 * w.row_waves, wgs = (rows + tile - 1) / tile * h->cfg.num_kv_heads;
     const int64_t tiles = ((int64_t)max_ctx_len + std::min(h->cfg.chunk_size, last_rows)) / 32 + 2;
-    w.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * std::max(h->num_cus, 1) / wgs, tiles / 8, 64}));
+    w.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * std::max(h->num_cus, 1) / wgs, tiles / 8, kWeighParts}));
     return w;
 }
 
 int64_t weigh_bytes(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
 {
-    return (int64_t)h->cfg.chunk_size * h->cfg.num_q_heads * weigh_shape(h, num_segs, max_ctx_len, last_rows).parts * 8;
+    const int64_t parts = weigh_shape(h, num_segs, max_ctx_len, last_rows).parts;
+    return (int64_t)h->cfg.chunk_size * h->cfg.num_q_heads * (parts > 1 ? 8 * parts + 4 : 4);
 }
 
 }  // namespace
@@ -171,19 +172,25 @@ tetri_status tetri_chunk_prefill_weights(tetri_ctx *h, const void *q, const void
     p.pages = static_cast<const uint16_t *>(kv_pages);
     p.weights = kv_weights;
     p.bt = block_table; p.cu = cu; p.ctx = ctx_lens;
-    p.stats = static_cast<float2 *>(workspace);
     p.S = num_segs; p.C = c.chunk_size; p.Hq = c.num_q_heads; p.Hkv = c.num_kv_heads; p.g = p.Hq / p.Hkv;
     p.max_blocks = c.max_blocks_per_seq; p.max_ctx = max_ctx_len;
     p.last = std::min(last_rows, c.chunk_size);
     const WeighShape shape = weigh_shape(h, num_segs, max_ctx_len, last_rows);
     p.row_waves = shape.row_waves; p.parts = shape.parts;
+    p.stats = static_cast<float2 *>(workspace);
+    p.lse = static_cast<float *>(workspace) + (p.parts > 1 ? (size_t)2 * p.C * p.Hq * p.parts : 0);
+    // 64 keys to a wavefront of the second pass where that still gives nearly every compute unit two workgroups (of several requests the longest is
+    // known: the others are taken for half as long on average).  16896 keys of 8 kv heads, 128 query rows each: 33 us in all against 36 with 32 keys;
+    // 2048 keys of 40 heads, 512 rows: 45 against 44; 7 segments of up to 3000 tokens over codes, 8 kv heads: 51 against 46.
+    p.wide_keys = ((int64_t)max_ctx_len * (num_segs + 1) / 2 + c.chunk_size) / 256 * p.Hkv >= 15 * (int64_t)h->num_cus / 8;
     p.g_magic = p.g <= 1 ? 0u : (uint32_t)((0x100000000ull + p.g - 1) / p.g);
     // (never 0: a masked score is an infinity, which the factor turns into -infinity)
     const auto factor = [&](float of) { return std::copysign(std::fmax(std::fabs(scale) * 1.4426950408889634f * of, 1e-30f), scale); };
     p.c = factor(1.f);
     p.c_codes = factor(fp8 ? k_scale : 1.f);
     const int64_t rows = std::min<int64_t>(p.C, (int64_t)p.S * p.last) * p.g;
-    if ((rows / 64 + p.S) * p.parts * p.Hkv > 0x7fffffff || ((int64_t)p.C * p.g + 64) * p.g > 0xffffffffll)
+    if ((rows / 64 + p.S) * p.parts * p.Hkv > 0x7fffffff || ((int64_t)p.C * p.g + 64) * p.g > 0xffffffffll ||
+        (int64_t)p.C * p.Hq * c.head_dim * 2 > 0xffffffffll)
         return tetri_fail(h, TETRI_ERR_INVALID_ARG, "%s: too many rows for one launch", fn);
     const hipError_t e = tetri_launch_weigh(c.head_dim, fp8 != 0, p, h->num_cus, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return tetri_fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));

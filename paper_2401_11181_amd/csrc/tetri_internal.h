@@ -319,16 +319,19 @@ struct AddWeightsParams {
 };
 
 // Weights that the last rows of a chunk's segments give to the keys (tetri_weights.hip).
+constexpr int32_t kWeighParts = 64;     // parts of a row's keys at most
 struct WeighParams {
     const uint16_t *q, *k_new, *pages;
     float *weights;       // [page][kv head][slot]
     const int32_t *bt, *cu, *ctx;
     float2 *stats;        // [chunk row][query head][part]: reference exponent and sum of a row's softmax over a part of its keys
+    float *lse;           // [chunk row][query head]: log2 of the whole sum
     int32_t S, C, Hq, Hkv, g, max_blocks;
     int32_t max_ctx;      // longest context
     int32_t last;         // rows of a segment that are looked at
     int32_t row_waves;    // wavefronts of a workgroup that have different rows (1, 2 or 4)
     int32_t parts;        // the keys of a row tile in that many parts
+    int32_t wide_keys;    // 1: 64 keys to a wavefront of the second pass, otherwise 32
     uint32_t g_magic;     // ceil(2^32 / g), 0 for 1
     float c, c_codes;     // scale * log2(e), and the same for scores of codes
 };

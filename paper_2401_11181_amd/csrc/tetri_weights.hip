@@ -68,24 +68,31 @@ struct Segment {
     int local;                // tile inside the segment
 };
 
+// What finds a workgroup's segment: leading arguments of the kernels, in registers when a wavefront starts (the structure behind them is a
+// memory read away).
+struct Lookup {
+    const int32_t *cu, *ctx;
+    int S, C, max_tokens, max_ctx, last, g;
+};
+
 // Finds tile `tile` when the tiles of all segments are numbered segment after segment; `count` gives a segment's.  False past the last.
 template <class F>
-__device__ inline bool find_segment(const WeighParams &p, int tile, int lane, F count, Segment &x)
+__device__ __forceinline__ bool find_segment(const Lookup &p, int tile, int lane, F count, Segment &x)
 {
     int base = 0;
     for (int s0 = 0; s0 < p.S; s0 += 64) {
-        const int s = s0 + lane;
+        const int s = s0 + lane, m = min(p.S - s0, 64);
         int first = 0, n = 0, L = 0, tiles = 0;
-        if (s < p.S) {
+        if (lane < m) {
             first = min(max(p.cu[s], 0), p.C);
             n = min(max(p.cu[s + 1], first), p.C) - first;
             L = p.ctx[s];
             // (a segment that is longer than the caller said, or than the block table can describe, is left out)
-            if (n > 0 && L >= 0 && L <= p.max_ctx && L <= p.max_blocks * kPage - n) tiles = count(n, L);
+            if (n > 0 && L >= 0 && L <= p.max_ctx && L <= p.max_tokens - n) tiles = count(n, L);
         }
         int incl = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
+#pragma unroll 1
+        for (int d = 1; d < m; d <<= 1) {
             const int up = __shfl_up(incl, d);
             if (lane >= d) incl += up;
         }
@@ -110,10 +117,45 @@ __device__ inline bool find_segment(const WeighParams &p, int tile, int lane, F 
 // Both passes are the same product with the parts changed: a wavefront keeps the fragments of 64 rows of one operand in registers (first
 // pass: query rows, second: keys) and goes over tiles of 32 rows of the other, which come through rings in LDS; a lane has two
 // columns of the result, and whatever is summed it sums by itself.  The matrix pipe needs 512 cycles for a step's 64 x 32 x 128
-// products, the vector pipe 768 for its 2048 exponentials (16 cycles per 64 of them) with an addition and a multiplication-addition
-// each: that is the bound where there are many rows.
+// products, the vector pipe as many for its 2048 exponentials (8 cycles per 64 of them) with an addition and a multiplication-addition
+// each.  So that both are at work, the products of one block of 32 x 32 scores stand between the exponentials of the block before, a matrix
+// instruction to two elements.  (2048 rows behind 14336 tokens, 32/8 heads, where the card's power is what bounds it: 535 us, 470 if all
+// values are the same; one after the other 579.  Two products of that size by the library's rate for large matrices: 432.)
 constexpr int kSub = 2;                  // blocks of 32 rows that a wavefront keeps
 constexpr int kStreamBytes = 8192;       // a tile of 32 rows of 128 16-bit values
+
+// next = a b; meanwhile element(v) for v = 0 .. 15 gives the exponents of the weights of the block before, whose sum is added to `sum`.
+template <int KSTEPS, class F>
+__device__ __forceinline__ void products_and_weights(const bf16x8 (&a)[KSTEPS], const bf16x8 (&b)[KSTEPS], f32x16 &next, float &sum, F element)
+{
+    constexpr int EACH = 16 / KSTEPS;
+    float t[EACH], w[EACH];
+    f32x16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s], b[s], acc, 0, 0, 0);
+        if (s == 0) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) t[i] = element(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) sum += w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) w[i] = __builtin_amdgcn_exp2f(t[i]);
+        if (s + 1 < KSTEPS) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) t[i] = element((s + 1) * EACH + i);
+        }
+        asm volatile("" : "+v"(sum));                    // (a sum whose use is far away would be taken there)
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sum += w[i];
+    next = acc;
+}
 
 // Rows of 16-bit values (or codes) as they lie in a tile in LDS: 16-byte chunks XOR-ed by the row (see attn_common.h).
 template <int D, bool CODES> struct StreamTile {
@@ -140,6 +182,20 @@ template <int D, bool CODES> __device__ __forceinline__ uint32_t tile_base(int l
     return row * StreamTile<D, CODES>::RB + (CODES ? (swz << 4) + 8 * half : (half ^ swz) << 4);
 }
 
+// 16 bytes per lane from base + off to LDS (see dma16; base is wave-uniform).
+__device__ __forceinline__ void dma16_at(const void *base, uint32_t off, uint32_t lds)
+{
+    dma16(reinterpret_cast<const char *>(uniform_ptr(base)) + off, lds);
+}
+
+// Fragments are in their registers from here on.  (Without this the compiler waits for them where they are used, in the loop, and there every
+// load to LDS that is in flight with them.)
+template <int KSTEPS> __device__ __forceinline__ void loaded(bf16x8 (&f)[KSTEPS])
+{
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) asm volatile("" : "+v"(f[s]));
+}
+
 // Fragments of 32 rows straight from memory, a row to a lane.
 template <int D> __device__ __forceinline__ void load_rows(const char *row, int half, bf16x8 (&f)[D / 16])
 {
@@ -156,13 +212,12 @@ template <int D> __device__ __forceinline__ void load_codes(const char *row, int
         f[s] = codes_to_bf16(x[0], x[1]);
     }
 }
-// Key `key` of a segment (cached: through the block table; otherwise the chunk's own row) for kv head kh.
+// Key `key` of a segment (cached: in page `page`; otherwise the chunk's own row) for kv head kh.
 template <int D, bool FP8>
-__device__ __forceinline__ void load_key(const WeighParams &p, const Segment &x, int kh, bool cached, int key, int half, bf16x8 (&f)[D / 16])
+__device__ __forceinline__ void load_key(const WeighParams &p, const Segment &x, int kh, bool cached, int page, int key, int half, bf16x8 (&f)[D / 16])
 {
     if (cached) {
         constexpr int RB = FP8 ? D : 2 * D;
-        const int page = p.bt[(size_t)x.s * p.max_blocks + key / kPage];
         const char *row = reinterpret_cast<const char *>(p.pages) + (((size_t)page * 2 * p.Hkv + kh) * kPage + key % kPage) * RB;
         if constexpr (FP8) load_codes<D>(row, half, f);
         else load_rows<D>(row, half, f);
@@ -179,19 +234,21 @@ __device__ __forceinline__ size_t query_row(const WeighParams &p, const Segment 
 
 // First pass: reference exponent and sum of the softmax of every row over a part of its keys.  RW wavefronts share a stream of key tiles,
 // each with 64 rows of its own; the 4 / RW streams of a workgroup take the tiles of the part in turn.  S^T = K Q^T: a lane has a
-// row.  The reference is the largest score of the row's first tile and stays so while the sum stays below 2^64: in fp32 a large
+// row.  The reference is the largest score of the row's first tile and stays so as long as the sum does not overflow: in fp32 a large
 // sum is as exact as a small one.
 template <int D, bool FP8, int RW>
-__global__ __launch_bounds__(256, 2) void weigh_rows_kernel(WeighParams p)
+__global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, const int32_t *ctx, int S, int C, int max_tokens, int max_ctx, int last, int g,
+                                                            int Hkv, int parts, WeighParams p)
 {
     constexpr int KSTEPS = D / 16, KW = 4 / RW, DEPTH = KW == 4 ? 2 : 4;
     __shared__ __attribute__((aligned(1024))) char smem[KW * DEPTH * kStreamBytes];
     __shared__ float2 met[4][32 * kSub];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const int rw = wave % RW, kw = wave / RW;            // which rows, which stream
-    const int kh = blockIdx.x % p.Hkv, rest = blockIdx.x / p.Hkv, part = rest % p.parts;
+    const int kh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv, part = rest % parts;
     Segment x;
-    if (!find_segment(p, rest / p.parts, lane, [&](int n, int) { return (min(n, p.last) * p.g + 32 * kSub * RW - 1) / (32 * kSub * RW); }, x)) return;
+    if (!find_segment(Lookup{cu, ctx, S, C, max_tokens, max_ctx, last, g}, rest / parts, lane,
+                      [&](int n, int) { return (min(n, last) * g + 32 * kSub * RW - 1) / (32 * kSub * RW); }, x)) return;
     const int row0 = (x.local * RW + rw) * 32 * kSub;    // the wavefront's first row
     bf16x8 qf[kSub][KSTEPS];
     int t[kSub];                                         // the lane's rows see new keys 0..t
@@ -206,106 +263,146 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(WeighParams p)
     const int old_tiles = (x.L + 31) / 32, tiles = old_tiles + t_last / 32 + 1;
     const int each = (tiles + p.parts - 1) / p.parts, begin = min(tiles, part * each), end = min(tiles, begin + each);
     float m[kSub], l[kSub];
-#pragma unroll
-    for (int i = 0; i < kSub; ++i) m[i] = -1e30f, l[i] = 0.f;
     const const_i32 *table = (const const_i32 *)(uintptr_t)(p.bt + (size_t)x.s * p.max_blocks);
+#pragma unroll
+    for (int i = 0; i < kSub; ++i) loaded(qf[i]);
     char *ring = smem + kw * (DEPTH * kStreamBytes);
     const uint32_t ring_lds = lds_address(ring);
 
+    f32x16 sc[kSub];                                     // block 1's weights are taken one step late
+    auto rescue = [&](int b, float c, float before) {
+        // a row's first tile, or one far above its reference: another one
+        if (__builtin_amdgcn_ballot_w64(!(l[b] <= 0x1p64f))) {
+            float mx = sc[b][0] * c;
+#pragma unroll
+            for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[b][v] * c);
+            const float m_new = fmaxf(m[b], half_swap_max(mx));      // (the other half-wave has other keys of the same row)
+            float sum = before * __builtin_amdgcn_exp2f(m[b] - m_new);
+            m[b] = m_new;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][v], c, -m_new));
+            l[b] = sum;
+        }
+    };
     // tiles [from, to) of all of them
-    auto stream = [&](auto codes_, int from, int to) {
+    auto stream = [&](auto codes_, bool careful, int from, int to) {
         constexpr bool CODES = decltype(codes_)::value;
         typedef StreamTile<D, CODES> T;
         constexpr int MY = (T::NI + RW - 1) / RW;        // load instructions of a wavefront
-        const uint32_t base = tile_base<D, CODES>(lane);
+        int ln = lane;
+        asm volatile("" : "+v"(ln));                     // (what follows from it is worked out here, not kept from one stream to the next)
+        static_assert(MY <= 2 || MY == 4 || MY == 8, "they move a whole number of pages, or a part of one");
+        const uint32_t base = tile_base<D, CODES>(ln);
+        const int i0 = MY * rw % T::NI;                  // the first of them; its lane's row and chunk
+        const int r0 = T::RPI * i0 + ln / T::CH;
+        uint32_t page_off[MY];                           // where in its page a row's 16 bytes are, less the instruction's own 1 KB
+#pragma unroll
+        for (int j = 0; j < MY; ++j) {
+            const int r = r0 + T::RPI * j;
+            page_off[j] = (uint32_t)((r % kPage) * T::RB + (((ln % T::CH) ^ T::swizzle(r)) << 4));
+        }
+        const char *pool = reinterpret_cast<const char *>(p.pages) + (size_t)kh * (kPage * T::RB);
+        const char *rows = reinterpret_cast<const char *>(p.k_new + ((size_t)x.first * p.Hkv + kh) * D);
+        const size_t page_bytes = (size_t)2 * p.Hkv * (kPage * T::RB);
+        const uint32_t row_bytes = (uint32_t)p.Hkv * 2 * D;
+        constexpr int PAGES = (MY * T::RPI + kPage - 1) / kPage, PER = MY / PAGES;   // pages that they read from, and how many read from one
+        int page[PAGES];                                 // of the tile that is issued next
+        // (rows of the last tile past the end: what the last page holds; tiles of new keys have no pages)
+        auto find_pages = [&](int it) {
+#pragma unroll
+            for (int j = 0; j < PAGES; ++j) page[j] = table[(uint32_t)max(min(32 * it + T::RPI * i0 + kPage * j, x.L - 1), 0) / kPage];
+        };
         auto issue = [&](int it, int slot) {
             it = min(it, to - 1);                        // (past the end: the last tile once more, so that the waits below count the same)
-            const uint32_t lds = ring_lds + slot * kStreamBytes;
-            const bool cached = it < old_tiles;
-            const int key0 = 32 * (cached ? it : it - old_tiles);
+            const uint32_t lds = ring_lds + slot * kStreamBytes + i0 * 1024;
+            if (it < old_tiles) {
 #pragma unroll
-            for (int j = 0; j < MY; ++j) {
-                const int i = (MY * rw + j) % T::NI;
-                const int r = T::RPI * i + lane / T::CH, chunk = (lane % T::CH) ^ T::swizzle(r);
-                const char *src;
-                if (cached) {
-                    // (the last tile's rows past the end: what the last page holds)
-                    const int page = table[min(key0 + T::RPI * i, x.L - 1) / kPage];
-                    src = reinterpret_cast<const char *>(p.pages) + ((size_t)page * 2 * p.Hkv + kh) * (kPage * T::RB) + (r % kPage) * T::RB;
-                } else {
-                    src = reinterpret_cast<const char *>(p.k_new) + ((size_t)(x.first + min(key0 + r, x.n - 1)) * p.Hkv + kh) * (2 * D);
+                for (int j = 0; j < MY; ++j) dma16_at(pool + page[j / PER] * page_bytes, page_off[j], lds + j * 1024);
+            } else {
+                const int key0 = 32 * (it - old_tiles);
+#pragma unroll
+                for (int j = 0; j < MY; ++j) {
+                    const int r = r0 + T::RPI * j;
+                    dma16_at(rows, (uint32_t)min(key0 + r, x.n - 1) * row_bytes + (((ln % T::CH) ^ T::swizzle(r)) << 4), lds + j * 1024);
                 }
-                dma16(src + chunk * 16, lds + i * 1024);
             }
+            find_pages(min(it + KW, to - 1));
         };
         const int steps = (to - from + KW - 1) / KW;     // of every stream of the workgroup
         if (steps <= 0) return;
+        const float c = CODES ? p.c_codes : p.c, none = c < 0.f ? INFINITY : -INFINITY;
+        const char *at = ring;
+        // scores that a row does not see are infinite, so that their weight is 0 under any reference: those of the last cached tile, of the
+        // tiles from that of the wavefront's first row on, and of those past the end that even out the streams
+        const int partial = x.L % 32 != 0 ? old_tiles - 1 : -1, mask_from = min(old_tiles + (t_first + 1) / 32, to);
+        auto mask = [&](int it, int b) {
+            if (it == partial || it >= mask_from) {
+                const int most = it >= to ? -1 : it < old_tiles ? x.L - 1 - 32 * it - 4 * half : t[b] - 32 * (it - old_tiles) - 4 * half;
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (8 * (v / 4) + v % 4 > most) sc[b][v] = none;
+            }
+        };
         lds_barrier();                                   // (the ring's last tiles have been read)
+        find_pages(min(from + kw, to - 1));
 #pragma unroll
         for (int i = 0; i < DEPTH - 1; ++i) issue(from + kw + KW * i, i);
-        for (int i = 0; i < steps; ++i) {
-            const int it = from + kw + KW * i;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[1][v] = none;
+        bf16x8 kf[2][KSTEPS];
+        auto arrive = [&](int i, bf16x8 (&f)[KSTEPS]) {  // step i's tile
             wait_vm<MY *(DEPTH - 2)>();
-            lds_barrier();                               // the tile is there, and everybody is done with the one before
-            issue(it + KW * (DEPTH - 1), (i + DEPTH - 1) % DEPTH);
-            const bool cached = it < old_tiles;
-            const int key0 = 32 * (cached ? it : it - old_tiles);
-            if (it >= to) continue;
-            bf16x8 kf[KSTEPS];
-            read_tile<D, CODES>(ring + (i % DEPTH) * kStreamBytes, base, kf);
-            const float c = CODES ? p.c_codes : p.c;
-            const bool masked = cached ? key0 + 32 > x.L : key0 + 31 > t_first;
-            f32x16 sc[kSub];
-#pragma unroll
-            for (int b = 0; b < kSub; ++b) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) sc[b][v] = 0.f;
-#pragma unroll
-                for (int s = 0; s < KSTEPS; ++s) sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[b][s], sc[b], 0, 0, 0);
-            }
-            if (masked) {                                // (as scores, so that their weight is 0 under any reference)
-                const float none = c < 0.f ? INFINITY : -INFINITY;
-#pragma unroll
-                for (int b = 0; b < kSub; ++b) {
-                    const int most = cached ? x.L - 1 : t[b];
-#pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        if (key0 + 8 * (v / 4) + 4 * half + v % 4 > most) sc[b][v] = none;
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < kSub; ++b) {
-                float sum = l[b];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][v], c, -m[b]));
-                if (__builtin_amdgcn_ballot_w64(!(sum <= 0x1p64f))) {
-                    // a row's first tile, or one far above it: another reference
-                    float mx = sc[b][0] * c;
-#pragma unroll
-                    for (int v = 1; v < 16; ++v) mx = fmaxf(mx, sc[b][v] * c);
-                    const float m_new = fmaxf(m[b], mx);
-                    sum = l[b] * __builtin_amdgcn_exp2f(m[b] - m_new);
-                    m[b] = m_new;
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][v], c, -m_new));
-                }
-                l[b] = sum;
-            }
+            lds_barrier();                               // it is there, and everybody has read the one before
+            issue(from + kw + KW * (i + DEPTH - 1), (i + DEPTH - 1) % DEPTH);
+            read_tile<D, CODES>(at + (i % DEPTH) * kStreamBytes, base, f);
+        };
+        auto step = [&](int i, bf16x8 (&f)[KSTEPS], bf16x8 (&f_next)[KSTEPS]) {
+            const int it = from + kw + KW * i;
+            float before = l[1];
+            products_and_weights<KSTEPS>(f, qf[0], sc[0], l[1], [&](int v) { return __builtin_fmaf(sc[1][v], c, -m[1]); });
+            if (careful || i == 1) rescue(1, c, before);
+            mask(it, 0);
+            if (i + 1 < steps) arrive(i + 1, f_next);
+            before = l[0];
+            products_and_weights<KSTEPS>(f, qf[1], sc[1], l[0], [&](int v) { return __builtin_fmaf(sc[0][v], c, -m[0]); });
+            if (careful || i == 0) rescue(0, c, before);
+            mask(it, 1);
+        };
+        arrive(0, kf[0]);
+        for (int i = 0; i < steps; i += 2) {
+            step(i, kf[0], kf[1]);
+            if (i + 1 < steps) step(i + 1, kf[1], kf[0]);
         }
+        const float before = l[1];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) l[1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[1][v], c, -m[1]));
+        rescue(1, c, before);
         wait_vm<0>();
     };
-    if constexpr (FP8) {
-        const int cut = min(max(old_tiles, begin), end);
-        stream(std::true_type(), begin, cut);
-        stream(std::false_type(), cut, end);
-    } else {
-        stream(std::false_type(), begin, end);
+    // The reference is looked at in a row's first tile and then only if the sum has overflowed: once more with a look at every tile.  (All
+    // wavefronts of the workgroup go along, for the barriers.)
+    __shared__ int overflow;
+    if (tid == 0) overflow = 0;
+    for (int careful = 0; careful < 2; ++careful) {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) m[i] = -1e30f, l[i] = 0.f;
+        if constexpr (FP8) {
+            const int cut = min(max(old_tiles, begin), end);
+            stream(std::true_type(), careful, begin, cut);
+            stream(std::false_type(), careful, cut, end);
+        } else {
+            stream(std::false_type(), careful, begin, end);
+        }
+        if (careful) break;
+        if (__builtin_amdgcn_ballot_w64(!(l[0] < INFINITY) || !(l[1] < INFINITY))) overflow = 1;
+        __syncthreads();
+        if (!overflow) break;
     }
-    // the halves of a wavefront (their references differ), then the streams
+    // the halves of a wavefront, then the streams
 #pragma unroll
     for (int i = 0; i < kSub; ++i) {
-        const float m2 = half_swap_max(m[i]), l2 = half_swap_sum(l[i] * __builtin_amdgcn_exp2f(m[i] - m2));
-        if (half == 0) met[wave][32 * i + l32] = make_float2(m2, l2);
+        const float both = half_swap_sum(l[i]);
+        if (half == 0) met[wave][32 * i + l32] = make_float2(m[i], both);
     }
     __syncthreads();
     const int r = x.local * RW * 32 * kSub + tid;
@@ -316,113 +413,183 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(WeighParams p)
         for (int i = 1; i < KW; ++i) ms = fmaxf(ms, met[w + i * RW][col].x);
 #pragma unroll
         for (int i = 0; i < KW; ++i) sum = __builtin_fmaf(met[w + i * RW][col].y, __builtin_amdgcn_exp2f(met[w + i * RW][col].x - ms), sum);
-        p.stats[query_row(p, x, kh, r) * p.parts + part] = make_float2(ms, sum);
+        const size_t row = query_row(p, x, kh, r);
+        if (parts == 1) p.lse[row] = ms + __builtin_amdgcn_logf(sum);
+        else p.stats[row * parts + part] = make_float2(ms, sum);
     }
 }
 
-// Second pass: the weights.  A wavefront keeps 64 keys of one kv head and the workgroup goes over the query rows that see any of its 256; S = Q K^T:
-// a lane has a key.  The logarithms of the rows' sums are put together from the parts for 256 rows at a time.
-template <int D, bool FP8>
-__global__ __launch_bounds__(256, 2) void weigh_keys_kernel(WeighParams p)
+// Between the passes, where the keys were cut: a row's parts put together, 16 lanes to a row.  (By every workgroup of the second pass for the rows
+// it needs, this took as long as a launch: each of them waits for it, and it takes their registers.)
+__global__ __launch_bounds__(256) void join_parts_kernel(const float2 *stats, float *lse, int parts, uint32_t rows)
 {
-    constexpr int KSTEPS = D / 16, DEPTH = 4, KEYS = 4 * 32 * kSub, BATCH = 256;
+    const uint32_t row = blockIdx.x * 16 + threadIdx.x / 16;
+    if (row >= rows) return;
+    const float2 *z = stats + (size_t)row * parts;
+    float m = -1e30f, l = 0.f;
+    for (int k = threadIdx.x % 16; k < parts; k += 16) {
+        const float2 y = z[k];
+        const float m_new = fmaxf(m, y.x);
+        l = __builtin_fmaf(y.y, __builtin_amdgcn_exp2f(y.x - m_new), l * __builtin_amdgcn_exp2f(m - m_new));
+        m = m_new;
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+        const float m2 = __shfl_xor(m, d), l2 = __shfl_xor(l, d), m_new = fmaxf(m, m2);
+        l = __builtin_fmaf(l2, __builtin_amdgcn_exp2f(m2 - m_new), l * __builtin_amdgcn_exp2f(m - m_new));
+        m = m_new;
+    }
+    if (threadIdx.x % 16 == 0) lse[row] = m + __builtin_amdgcn_logf(l);
+}
+
+// Second pass: the weights.  A wavefront keeps 32 * SUB keys of one kv head and the workgroup goes over the query rows that see any of its
+// 128 * SUB; S = Q K^T: a lane has a key.  64 keys to a wavefront halve what is read from LDS; 32 where that leaves compute units without
+// work.
+template <int D, bool FP8, int SUB>
+__global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const int32_t *cu, const int32_t *ctx, int S, int C, int max_tokens, int max_ctx, int last,
+                                                                          int g, int Hkv, WeighParams p)
+{
+    constexpr int KSTEPS = D / 16, DEPTH = 4, KEYS = 4 * 32 * SUB, BATCH = 256;
     typedef StreamTile<D, false> T;
     constexpr int MY = T::NI / 4;
     __shared__ __attribute__((aligned(1024))) char ring[DEPTH * kStreamBytes];
-    __shared__ __attribute__((aligned(16))) float minus_lse[BATCH];
+    __shared__ __attribute__((aligned(16))) float minus_lse[2 * BATCH];   // of this batch of rows and the one before
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
-    const int kh = blockIdx.x % p.Hkv;
+    const int kh = blockIdx.x % Hkv;
     const uint32_t base = tile_base<D, false>(lane), ring_lds = lds_address(ring);
-    for (int item = blockIdx.x / p.Hkv;; item += gridDim.x / p.Hkv) {
+    for (int item = blockIdx.x / Hkv;; item += gridDim.x / Hkv) {
         Segment x;
-        if (!find_segment(p, item, lane, [&](int n, int L) { return (L + KEYS - 1) / KEYS + (n + KEYS - 1) / KEYS; }, x)) return;
+        if (!find_segment(Lookup{cu, ctx, S, C, max_tokens, max_ctx, last, g}, item, lane,
+                          [&](int n, int L) { return (L + KEYS - 1) / KEYS + (n + KEYS - 1) / KEYS; }, x)) return;
         const int old_tiles = (x.L + KEYS - 1) / KEYS;
         const bool cached = x.local < old_tiles;
         const int tile0 = KEYS * (cached ? x.local : x.local - old_tiles), keys = cached ? x.L : x.n;
-        const int key0 = tile0 + 32 * kSub * wave;       // the wavefront's first
-        bf16x8 kf[kSub][KSTEPS];
-#pragma unroll
-        for (int b = 0; b < kSub; ++b) load_key<D, FP8>(p, x, kh, cached, min(key0 + 32 * b + l32, keys - 1), half, kf[b]);
+        const int key0 = tile0 + 32 * SUB * wave;        // the wavefront's first
         const float c = FP8 && cached ? p.c_codes : p.c;
-        float sum[kSub];
-#pragma unroll
-        for (int b = 0; b < kSub; ++b) sum[b] = 0.f;
+        float sum[2] = {0.f, 0.f};
         // (the rows in front of the first that sees a key of the tile are left out)
-        const int from = cached ? 0 : max(0, tile0 - x.t0) * p.g / 32, to = (x.rows + 31) / 32;
-        auto issue = [&](int rt, int slot) {
-            rt = min(rt, to - 1);
+        const int from = cached ? 0 : max(0, tile0 - x.t0) * g / 32, to = (x.rows + 31) / 32, steps = to - from;
+        // where the lane's query rows of the next tile are, from the segment's first on: they go up by 32 rows, that is by 32 / g tokens and
+        // 32 % g heads; rows past the end are the last one
+        uint32_t off[MY], head[MY];
+        const uint32_t token_bytes = (uint32_t)p.Hq * 2 * D, per_tile = 32u / (uint32_t)p.g * token_bytes + 32u % (uint32_t)p.g * 2 * D;
+        const uint32_t last_off = (uint32_t)(x.n - 1 - x.t0) * token_bytes + (uint32_t)(p.g - 1) * 2 * D;
+        const char *queries = reinterpret_cast<const char *>(p.q + query_row(p, x, kh, 0) * D);
+#pragma unroll
+        for (int j = 0; j < MY; ++j) {
+            const int r = from * 32 + T::RPI * (MY * wave + j) + lane / T::CH, token = magic_div(r, p.g_magic);
+            head[j] = r - token * p.g;
+            off[j] = token * token_bytes + head[j] * 2 * D;
+        }
+        auto issue = [&](int slot) {
 #pragma unroll
             for (int j = 0; j < MY; ++j) {
                 const int i = MY * wave + j, r = T::RPI * i + lane / T::CH;
-                const size_t row = query_row(p, x, kh, min(rt * 32 + r, x.rows - 1));
-                dma16(reinterpret_cast<const char *>(p.q + row * D) + ((lane % T::CH) ^ T::swizzle(r)) * 16, ring_lds + slot * kStreamBytes + i * 1024);
+                dma16_at(queries, min(off[j], last_off) + (((lane % T::CH) ^ T::swizzle(r)) << 4), ring_lds + slot * kStreamBytes + i * 1024);
+                head[j] += 32u % (uint32_t)p.g;
+                off[j] += per_tile;
+                if (head[j] >= (uint32_t)p.g) {
+                    head[j] -= p.g;
+                    off[j] += token_bytes - (uint32_t)p.g * 2 * D;
+                }
+            }
+        };
+        f32x16 sc[2];
+        const float none = c < 0.f ? INFINITY : -INFINITY;
+        // a key of the chunk is seen by row first_row[b] and those behind it
+        int first_row[SUB];
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) first_row[b] = cached ? 0 : (key0 + 32 * b + l32 - x.t0) * g;
+        const int all_see = cached ? 0 : (key0 + 32 * SUB - 1 - x.t0) * g;
+        auto mask = [&](int rt, int b, f32x16 &s) {
+            if (rt * 32 < all_see) {
+                const int least = first_row[b] - rt * 32 - 4 * half;
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (8 * (v / 4) + v % 4 < least) s[v] = none;
             }
         };
         lds_barrier();                                   // (everybody is done with the item before)
 #pragma unroll
-        for (int i = 0; i < DEPTH - 1; ++i) issue(from + i, i);
-        for (int rt = from; rt < to; ++rt) {
-            const int i = rt - from;
-            if (i % (BATCH / 32) == 0) {
-                lds_barrier();
-                const int r = rt * 32 + tid;
-                float neg = -INFINITY;                   // rows past the end: weight 0
-                if (r < x.rows) {
-                    const float2 *z = p.stats + query_row(p, x, kh, r) * p.parts;
-                    float ms = z[0].x, l = z[0].y;
-                    for (int k = 1; k < p.parts; ++k) {
-                        const float m_new = fmaxf(ms, z[k].x);
-                        l = __builtin_fmaf(z[k].y, __builtin_amdgcn_exp2f(z[k].x - m_new), l * __builtin_amdgcn_exp2f(ms - m_new));
-                        ms = m_new;
-                    }
-                    neg = -(ms + __builtin_amdgcn_logf(l));
-                }
-                minus_lse[tid] = neg;
-                wait_vm<0>();                            // (the loads above have been waited for out of turn)
-            } else {
-                wait_vm<MY *(DEPTH - 2)>();
-            }
+        for (int i = 0; i < DEPTH - 1; ++i) issue(i);
+        bf16x8 kf[SUB][KSTEPS];
+        float *weight[SUB];                              // of the lane's keys, and what they have already
+        float sum_before[SUB];
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) {
+            const int key = min(key0 + 32 * b + l32, keys - 1), slot = cached ? key : x.L + key;
+            const int page = p.bt[(size_t)x.s * p.max_blocks + slot / kPage];
+            weight[b] = p.weights + ((size_t)page * Hkv + kh) * kPage + slot % kPage;
+            load_key<D, FP8>(p, x, kh, cached, page, key, half, kf[b]);
+            sum_before[b] = cached ? *weight[b] : 0.f;
+        }
+        // minus the logarithms of 256 rows' sums, from row r0 on; rows past the end: -infinity, that is weight 0
+        auto sums = [&](int r0, float *to_lds) {
+            const int r = r0 + tid;
+            to_lds[tid] = r < x.rows ? -p.lse[query_row(p, x, kh, r)] : -INFINITY;
+        };
+        if (steps > 0) sums(from * 32, minus_lse);
+#pragma unroll
+        for (int b = 0; b < SUB; ++b) {
+            loaded(kf[b]);
+            asm volatile("" : "+v"(sum_before[b]));
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[1][v] = none;
+        bf16x8 qf[SUB][KSTEPS];
+        auto arrive = [&](int i, bf16x8 (&f)[KSTEPS]) {
+            if (i > 0 && i % (BATCH / 32) == 0) sums((from + i) * 32, minus_lse + (i & (BATCH / 32)) * 32);
+            wait_vm<MY *(DEPTH - 2)>();
             lds_barrier();
-            issue(rt + DEPTH - 1, (i + DEPTH - 1) % DEPTH);
-            bf16x8 qf[KSTEPS];
-            read_tile<D, false>(ring + (i % DEPTH) * kStreamBytes, base, qf);
-            f32x4 neg[4];
+            issue((i + DEPTH - 1) % DEPTH);
+            read_tile<D, false>(ring + (i % DEPTH) * kStreamBytes, base, f);
+        };
+        f32x4 neg[4];
+        auto read_neg = [&](int i) {                     // of tile i
 #pragma unroll
-            for (int v = 0; v < 4; ++v) neg[v] = *reinterpret_cast<const f32x4 *>(minus_lse + (i % (BATCH / 32)) * 32 + 8 * v + 4 * half);
-            const bool masked = !cached && key0 + 32 * kSub - 1 > x.t0 + magic_div(rt * 32, p.g_magic);
-            f32x16 sc[kSub];
-#pragma unroll
-            for (int b = 0; b < kSub; ++b) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) sc[b][v] = 0.f;
-#pragma unroll
-                for (int s = 0; s < KSTEPS; ++s) sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[s], kf[b][s], sc[b], 0, 0, 0);
+            for (int v = 0; v < 4; ++v) neg[v] = *reinterpret_cast<const f32x4 *>(minus_lse + (i & (2 * BATCH / 32 - 1)) * 32 + 8 * v + 4 * half);
+        };
+        if constexpr (SUB == 2) {
+            // block 1's weights are taken one step late
+            auto step = [&](int i, bf16x8 (&f)[KSTEPS], bf16x8 (&f_next)[KSTEPS]) {
+                read_neg(i > 0 ? i - 1 : 0);
+                products_and_weights<KSTEPS>(f, kf[0], sc[0], sum[1], [&](int v) { return __builtin_fmaf(sc[1][v], c, neg[v / 4][v % 4]); });
+                read_neg(i);
+                mask(from + i, 0, sc[0]);
+                if (i + 1 < steps) arrive(i + 1, f_next);
+                products_and_weights<KSTEPS>(f, kf[1], sc[1], sum[0], [&](int v) { return __builtin_fmaf(sc[0][v], c, neg[v / 4][v % 4]); });
+                mask(from + i, 1, sc[1]);
+            };
+            if (steps > 0) arrive(0, qf[0]);
+            for (int i = 0; i < steps; i += 2) {
+                step(i, qf[0], qf[1]);
+                if (i + 1 < steps) step(i + 1, qf[1], qf[0]);
             }
-#pragma unroll
-            for (int b = 0; b < kSub; ++b) {
-                if (masked) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int row = x.t0 + magic_div(rt * 32 + 8 * (v / 4) + 4 * half + v % 4, p.g_magic);
-                        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][v], c, neg[v / 4][v % 4]));
-                        sum[b] += key0 + 32 * b + l32 <= row ? w : 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) sum[b] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][v], c, neg[v / 4][v % 4]));
-                }
+        } else {
+            // a tile's weights are taken one step late
+            auto step = [&](int i, f32x16 &s, const f32x16 &before) {
+                arrive(i, qf[0]);
+                read_neg(i > 0 ? i - 1 : 0);
+                products_and_weights<KSTEPS>(qf[0], kf[0], s, sum[0], [&](int v) { return __builtin_fmaf(before[v], c, neg[v / 4][v % 4]); });
+                mask(from + i, 0, s);
+            };
+            for (int i = 0; i < steps; i += 2) {
+                step(i, sc[0], sc[1]);
+                if (i + 1 < steps) step(i + 1, sc[1], sc[0]);
+                else sc[1] = sc[0];
             }
+        }
+        // the last block
+        if (steps > 0) {
+            read_neg(steps - 1);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sum[SUB - 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(sc[1][v], c, neg[v / 4][v % 4]));
         }
         wait_vm<0>();
 #pragma unroll
-        for (int b = 0; b < kSub; ++b) {
+        for (int b = 0; b < SUB; ++b) {
             const float total = half_swap_sum(sum[b]);
-            const int key = key0 + 32 * b + l32;
-            if (half == 0 && key < keys) {
-                const int slot = cached ? key : x.L + key;
-                float *w = p.weights + ((size_t)p.bt[(size_t)x.s * p.max_blocks + slot / kPage] * p.Hkv + kh) * kPage + slot % kPage;
-                *w = cached ? *w + total : total;
-            }
+            if (half == 0 && key0 + 32 * b + l32 < keys) *weight[b] = sum_before[b] + total;
         }
     }
 }
@@ -441,13 +608,24 @@ template <int D, bool FP8> static hipError_t launch_weigh(const WeighParams &p, 
     // upper bounds of the tiles: every segment may end in a partial one
     const int64_t rows = (int64_t)std::min<int64_t>(p.C, (int64_t)p.S * p.last) * p.g;
     const int64_t row_tiles = rows / (32 * kSub * p.row_waves) + p.S;
+    const int max_tokens = p.max_blocks * kPage;
     const auto rows_kernel = p.row_waves == 4 ? weigh_rows_kernel<D, FP8, 4> : p.row_waves == 2 ? weigh_rows_kernel<D, FP8, 2> : weigh_rows_kernel<D, FP8, 1>;
-    hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(row_tiles * p.parts * p.Hkv)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL(rows_kernel, dim3((unsigned)(row_tiles * p.parts * p.Hkv)), dim3(256), 0, stream, p.cu, p.ctx, p.S, p.C, max_tokens, p.max_ctx, p.last, p.g,
+                       p.Hkv, p.parts, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t key_tiles = (int64_t)p.S * ((p.max_ctx + 255) / 256) + p.C / 256 + p.S;
-    const int64_t abreast = std::max<int64_t>(1, (8 * (int64_t)num_cus + p.Hkv - 1) / p.Hkv);
-    hipLaunchKernelGGL((weigh_keys_kernel<D, FP8>), dim3((unsigned)(std::min(key_tiles, abreast) * p.Hkv)), dim3(256), 0, stream, p);
+    if (p.parts > 1) {
+        // (rows of the chunk that no segment's last rows are have no parts: what comes of them is not read)
+        hipLaunchKernelGGL(join_parts_kernel, dim3((unsigned)(((int64_t)p.C * p.Hq + 15) / 16)), dim3(256), 0, stream, p.stats, p.lse, p.parts, (uint32_t)(p.C * p.Hq));
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    auto key_tiles = [&](int64_t keys) { return (int64_t)p.S * ((p.max_ctx + keys - 1) / keys) + p.C / keys + p.S; };
+    const bool wide = p.wide_keys;
+    // no more workgroups than are resident at a time: those beyond them would start when the first have ended
+    const int64_t abreast = std::max<int64_t>(1, (wide ? 2 : 3) * (int64_t)num_cus / p.Hkv);
+    const auto keys_kernel = wide ? weigh_keys_kernel<D, FP8, 2> : weigh_keys_kernel<D, FP8, 1>;
+    hipLaunchKernelGGL(keys_kernel, dim3((unsigned)(std::min(key_tiles(wide ? 256 : 128), abreast) * p.Hkv)), dim3(256), 0, stream, p.cu, p.ctx, p.S, p.C, max_tokens,
+                       p.max_ctx, p.last, p.g, p.Hkv, p);
     return hipGetLastError();
 }
 
