@@ -172,90 +172,124 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
     }
 }
 
-// The moves in place.  A token's row of K (or V) of one kv head goes 16 bytes to a lane.  Two kinds:
+// The moves in place.  A token's row of K and of V goes 16 bytes to a lane.  Two kinds:
 //   * to the holes from behind the new end (slots n and up): no other move writes what it reads or reads what it writes, so
-//     all of them may run at once;
+//     all of them may run at once.  A workgroup has 256 slots of one kv head: it looks up the pages of those that get another
+//     token, a lane each, and moves just these, as many rows of both K and V at a time as keep the memory busy;
 //   * those that have to do with the last r slots [n - r, n): what a hole takes from there, and the newest tokens that come there.  Slot n - r + i
 //     may be read by two moves (by a hole's, and where e < r by that of slot n - r + i - e) before it is written.  One
-//     workgroup goes over these slots in order: it reads a stretch of slots for the holes and the tokens that come into the
+//     workgroup for K and one for V goes over these slots in order: it reads a stretch of slots for the holes and the tokens that come into the
 //     stretch, waits until all its reads have returned, and writes.  What it reads later lies behind what it has written.
+// Neighbouring workgroups have different kv heads of the same slots: what is under way at a time lies in few pages.
 constexpr int kCompactThreads = 256, kBack = 1024;
 
 template <int RB>      // bytes of a row
-__global__ __launch_bounds__(kCompactThreads) void compact_kernel(CompactParams p, int tiles)
+__global__ __launch_bounds__(kCompactThreads) void compact_kernel(const int32_t *ctx, const int32_t *bt, const int32_t *slots, int max_blocks, int Hkv, int keep,
+                                                                  int recent, int tiles, char *pages, float *weights)
 {
-    constexpr int LPR = RB / 16, STEP = kCompactThreads / LPR, ROWS = 4, TILE = ROWS * STEP;
+    constexpr int LPR = RB / 16, STEP = kCompactThreads / LPR, ROWS = 4, STRETCH = ROWS * STEP;
     __shared__ int32_t hole[kBack];
-    const int tid = threadIdx.x, lane_row = tid / LPR, chunk = tid % LPR;
-    int id = blockIdx.x;
-    const int tile = id % (tiles + 1);
-    id /= tiles + 1;
-    const int kv = id % 2;
-    id /= 2;
-    const int kh = id % p.Hkv, b = id / p.Hkv;
-    const int L = min(max(p.ctx[b], 0), p.max_blocks * kPage), n = min(L, p.keep), r = min(p.recent, n), heavy = n - r, e = L - n;
+    __shared__ int32_t moves[kCompactThreads][3];        // pages from and to, slots in them
+    __shared__ int32_t wave_moves[kCompactThreads / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lane_row = tid / LPR, chunk = tid % LPR;
+    const int rest = blockIdx.x / Hkv, kh = blockIdx.x - rest * Hkv, b = rest / (tiles + 2), tile = rest - b * (tiles + 2) - 2;
+    const int L = min(max(ctx[b], 0), max_blocks * kPage), n = min(L, keep), r = min(recent, n), heavy = n - r, e = L - n;
     if (e == 0) return;
-    const int32_t *map = p.slots + ((size_t)b * p.Hkv + kh) * p.keep, *row = p.bt + (size_t)b * p.max_blocks;
-    auto place = [&](int slot) -> size_t {               // of a slot among all (page, kv head, slot)
-        return ((size_t)row[slot / kPage] * p.Hkv + kh) * kPage + slot % kPage;
+    const int32_t *map = slots + ((size_t)b * Hkv + kh) * keep, *row = bt + (size_t)b * max_blocks;
+    auto data = [&](int page, int slot, int kv) -> char * {
+        return pages + ((((size_t)page * 2 + kv) * Hkv + kh) * kPage + slot) * RB + chunk * 16;
     };
-    auto data = [&](int slot) -> char * {
-        return p.pages + ((((size_t)row[slot / kPage] * 2 + kv) * p.Hkv + kh) * kPage + slot % kPage) * RB + chunk * 16;
-    };
-    auto ld = [&](int slot) -> u32x4 { return *reinterpret_cast<global_u32x4 *>((uintptr_t)data(slot)); };
-    auto st = [&](int slot, u32x4 v) { *reinterpret_cast<global_u32x4_w *>((uintptr_t)data(slot)) = v; };
-    const bool weight = kv == 0 && chunk == 0;           // these lanes move the weights as well
-    if (tile < tiles) {
-        int src[ROWS];
-        u32x4 v[ROWS];
-        float w[ROWS];
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i) {
-            const int to = tile * TILE + i * STEP + lane_row;
-            src[i] = to < heavy ? map[to] : -1;
-            if (src[i] < n || src[i] >= L) src[i] = -1;
+    auto ld = [&](int page, int slot, int kv) -> u32x4 { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(data(page, slot, kv))); };
+    auto st = [&](int page, int slot, int kv, u32x4 v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(data(page, slot, kv))); };
+    auto weight = [&](int page, int slot) -> float & { return weights[((size_t)page * Hkv + kh) * kPage + slot]; };
+    if (tile >= 0) {
+        const int to = tile * kCompactThreads + tid;
+        const int from = to < heavy ? map[to] : -1;
+        const bool move = from >= n && from < L;
+        const unsigned long long moved = __ballot(move);
+        if (lane == 0) wave_moves[wave] = __popcll(moved);
+        int pf = 0, pt = 0;
+        float w = 0.f;
+        if (move) {
+            pf = row[from / kPage];
+            pt = row[to / kPage];
+            w = weight(pf, from % kPage);
         }
+        __syncthreads();
+        int at = __popcll(moved & ((1ull << lane) - 1)), count = 0;
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            if (src[i] >= 0) {
-                v[i] = ld(src[i]);
-                if (weight) w[i] = p.weights[place(src[i])];
+        for (int i = 0; i < kCompactThreads / 64; ++i) {
+            if (i < wave) at += wave_moves[i];
+            count += wave_moves[i];
+        }
+        if (move) {
+            moves[at][0] = pf;
+            moves[at][1] = pt;
+            moves[at][2] = from % kPage | to % kPage << 16;
+            weight(pt, to % kPage) = w;
+        }
+        __syncthreads();
+        for (int m0 = 0; m0 < count; m0 += STRETCH) {
+            u32x4 v[ROWS][2];
+            int page_to[ROWS], slot_to[ROWS];
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const int m = m0 + i * STEP + lane_row;
+                slot_to[i] = -1;
+                if (m < count) {
+                    const int page = moves[m][0], s = moves[m][2];
+                    page_to[i] = moves[m][1];
+                    slot_to[i] = s >> 16;
+                    v[i][0] = ld(page, s & 0xffff, 0);
+                    v[i][1] = ld(page, s & 0xffff, 1);
+                }
             }
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-            if (src[i] >= 0) {
-                const int to = tile * TILE + i * STEP + lane_row;
-                st(to, v[i]);
-                if (weight) p.weights[place(to)] = w[i];
-            }
+            for (int i = 0; i < ROWS; ++i)
+                if (slot_to[i] >= 0) {
+                    st(page_to[i], slot_to[i], 0, v[i][0]);
+                    st(page_to[i], slot_to[i], 1, v[i][1]);
+                }
+        }
         return;
     }
+    const int kv = tile + 2;
+    const bool weighs = kv == 0 && chunk == 0;           // these lanes move the weights as well
     for (int base = 0; base < r; base += kBack) {
         const int many = min(r - base, kBack);
         __syncthreads();
         for (int i = tid; i < many; i += kCompactThreads) hole[i] = -1;
         __syncthreads();
-        for (int i = tid; i < heavy; i += kCompactThreads) {
-            const int at = map[i] - heavy - base;
-            if (at >= 0 && at < many) hole[at] = i;
+        for (int i0 = tid; i0 < heavy; i0 += 16 * kCompactThreads) {
+            int at[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) at[k] = map[min(i0 + k * kCompactThreads, heavy - 1)];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int i = i0 + k * kCompactThreads, x = at[k] - heavy - base;
+                if (i < heavy && x >= 0 && x < many) hole[x] = i;
+            }
         }
         __syncthreads();
-        for (int t0 = 0; t0 < many; t0 += TILE) {
+        for (int t0 = 0; t0 < many; t0 += STRETCH) {
             u32x4 old[ROWS], now[ROWS];
             float w_old[ROWS], w_now[ROWS];
-            int to[ROWS], at[ROWS];
+            int to[ROWS], at[ROWS], page[ROWS], page_to[ROWS];
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
                 const int x = t0 + i * STEP + lane_row;
                 at[i] = x < many ? heavy + base + x : -1;
                 to[i] = x < many ? hole[x] : -1;
-                if (to[i] >= 0) {
-                    old[i] = ld(at[i]);
-                    if (weight) w_old[i] = p.weights[place(at[i])];
-                }
                 if (at[i] >= 0) {
-                    now[i] = ld(at[i] + e);
-                    if (weight) w_now[i] = p.weights[place(at[i] + e)];
+                    page[i] = row[at[i] / kPage];
+                    page_to[i] = row[max(to[i], 0) / kPage];
+                    const int page_now = row[(at[i] + e) / kPage];
+                    if (to[i] >= 0) {
+                        old[i] = ld(page[i], at[i] % kPage, kv);
+                        if (weighs) w_old[i] = weight(page[i], at[i] % kPage);
+                    }
+                    now[i] = ld(page_now, (at[i] + e) % kPage, kv);
+                    if (weighs) w_now[i] = weight(page_now, (at[i] + e) % kPage);
                 }
             }
             wait_vm<0>();
@@ -263,12 +297,12 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(CompactParams 
 #pragma unroll
             for (int i = 0; i < ROWS; ++i) {
                 if (to[i] >= 0) {
-                    st(to[i], old[i]);
-                    if (weight) p.weights[place(to[i])] = w_old[i];
+                    st(page_to[i], to[i] % kPage, kv, old[i]);
+                    if (weighs) weight(page_to[i], to[i] % kPage) = w_old[i];
                 }
                 if (at[i] >= 0) {
-                    st(at[i], now[i]);
-                    if (weight) p.weights[place(at[i])] = w_now[i];
+                    st(page[i], at[i] % kPage, kv, now[i]);
+                    if (weighs) weight(page[i], at[i] % kPage) = w_now[i];
                 }
             }
         }
@@ -292,10 +326,11 @@ hipError_t tetri_launch_select(const SelectParams &p, hipStream_t stream)
 
 template <int RB> static hipError_t launch_compact(const CompactParams &p, hipStream_t stream)
 {
-    const int rows = 4 * kCompactThreads / (RB / 16), tiles = (p.keep + rows - 1) / rows;
-    const int64_t wgs = (int64_t)p.B * p.Hkv * 2 * (tiles + 1);
+    const int tiles = (p.keep - p.recent + kCompactThreads - 1) / kCompactThreads;
+    const int64_t wgs = (int64_t)p.B * p.Hkv * (tiles + 2);
     if (wgs > 0x7fffffff) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((compact_kernel<RB>), dim3((unsigned)wgs), dim3(kCompactThreads), 0, stream, p, tiles);
+    hipLaunchKernelGGL((compact_kernel<RB>), dim3((unsigned)wgs), dim3(kCompactThreads), 0, stream, p.ctx, p.bt, p.slots, p.max_blocks, p.Hkv, p.keep, p.recent, tiles,
+                       p.pages, p.weights);
     return hipGetLastError();
 }
 

@@ -245,8 +245,8 @@ tetri_status tetri_kv_compact(tetri_ctx *h, const int32_t *slots, const int32_t 
     if (st == TETRI_OK) st = check_device(h, fn);
     if (st != TETRI_OK) return st;
     CompactParams p = {slots, block_table, ctx_lens, static_cast<char *>(kv_pages), kv_weights, num_reqs, h->cfg.num_kv_heads, h->cfg.max_blocks_per_seq, keep, recent};
-    // (a workgroup moves 64 rows or more of K or V of one kv head)
-    if ((int64_t)num_reqs * h->cfg.num_kv_heads * 2 * (keep / 64 + 2) > 0x7fffffff)
+    // (a workgroup has 256 slots of one kv head)
+    if ((int64_t)num_reqs * h->cfg.num_kv_heads * (keep / 256 + 3) > 0x7fffffff)
         return tetri_fail(h, TETRI_ERR_INVALID_ARG, "%s: too many tokens for one launch", fn);
     const hipError_t e = tetri_launch_compact(h->cfg.head_dim * (fp8 ? 1 : 2), p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return tetri_fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
