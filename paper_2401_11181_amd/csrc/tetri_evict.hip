@@ -13,25 +13,42 @@ namespace {
 
 using namespace tetri_dev;
 
-constexpr int kSelectThreads = 1024, kDigits = 2048;
+constexpr int kDigits = 2048, kCandidates = 1024, kCompared = 128;
+
+// Value of another lane (0 where there is none, or in rows that `rows` leaves out), without a trip through LDS.
+template <int CTRL, int ROWS = 15> __device__ __forceinline__ int dpp(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 15, false); }
+
+// Sum over this lane and those in front of it.
+__device__ __forceinline__ int wave_scan(int x)
+{
+    x += dpp<0x111>(x);                                  // one, two, four and eight lanes up inside a row of 16
+    x += dpp<0x112>(x);
+    x += dpp<0x114>(x);
+    x += dpp<0x118>(x);
+    x += dpp<0x142, 10>(x);                              // the last lane of the row before to rows 1 and 3
+    x += dpp<0x143, 12>(x);                              // lane 31 to rows 2 and 3
+    return x;
+}
+// All bits of the eight lanes of a group.
+__device__ __forceinline__ uint32_t or_eight(uint32_t x)
+{
+    x |= (uint32_t)dpp<0xB1>((int)x);                    // neighbours, pairs, then the two halves (all lanes of a half hold the same by now)
+    x |= (uint32_t)dpp<0x4E>((int)x);
+    return x | (uint32_t)dpp<0x141>((int)x);
+}
 
 // Sum over the threads in front of this one; `total`: of all.
-__device__ inline int block_scan(int x, int *wave_sums, int &total)
+template <int THREADS> __device__ __forceinline__ int block_scan(int x, int *wave_sums, int &total)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int incl = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int up = __shfl_up(incl, d);
-        if (lane >= d) incl += up;
-    }
+    const int incl = wave_scan(x);
     __syncthreads();                                     // (everybody is done with an earlier scan's sums)
     if (lane == 63) wave_sums[wave] = incl;
     __syncthreads();
     int before = 0;
     total = 0;
 #pragma unroll
-    for (int i = 0; i < kSelectThreads / 64; ++i) {
+    for (int i = 0; i < THREADS / 64; ++i) {
         if (i < wave) before += wave_sums[i];
         total += wave_sums[i];
     }
@@ -46,10 +63,236 @@ __device__ __forceinline__ uint32_t ordered(float w)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// A workgroup per (request, kv head).  The smallest kept weight is found digit by digit (11, 11 and 10 bits, from the top), each by a
-// histogram of the weights that agree with the digits so far; then every slot's bit is known, and the map follows from the counts
-// of bits in front of each word.
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
+// A histogram's additions.  Additions to one word of LDS come one after the other: so there are COPIES of every digit's count, next to each other,
+// for a quarter of the lanes each where there are four; and weights of 0, of which there may be many, are counted by each lane for itself.
+// (32768 weights, 16 wavefronts: 20000 cycles with one copy.)
+constexpr uint32_t kZero = 0x80000000u;                  // ordered(0)
+template <int COPIES> __device__ __forceinline__ void count_digit(uint32_t *hist, uint32_t u, int shift, uint32_t digits, bool in, int &zeros)
+{
+    if (in && u == kZero) ++zeros;
+    if (in && u != kZero) atomicAdd(&hist[((u >> shift) & digits) * COPIES + threadIdx.x % COPIES], 1u);
+}
+template <int COPIES> __device__ __forceinline__ void count_zeros(uint32_t *hist, int shift, uint32_t digits, int zeros)
+{
+    if (zeros != 0) atomicAdd(&hist[((kZero >> shift) & digits) * COPIES + threadIdx.x % COPIES], (uint32_t)zeros);
+}
+template <int THREADS, int COPIES> __device__ __forceinline__ void clear_digits(uint32_t *hist)
+{
+    for (int i = threadIdx.x; i < kDigits * COPIES / 4; i += THREADS) reinterpret_cast<uint4 *>(hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+// Where the want-th largest is, from the largest digit down: its digit, how many are wanted of that digit, and how many there are.
+template <int THREADS, int COPIES> __device__ __forceinline__ void find_digit(const uint32_t *hist, int want, int *wave_sums, int (&found)[3])
+{
+    constexpr int MINE = kDigits / THREADS;
+    const int top = kDigits - 1 - MINE * threadIdx.x;    // this thread's digits: top, top - 1, ...
+    int n[MINE], sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) {
+        if constexpr (COPIES == 4) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(hist + 4 * (top - i));
+            n[i] = (int)(x.x + x.y + x.z + x.w);
+        } else {
+            n[i] = (int)hist[top - i];
+        }
+        sum += n[i];
+    }
+    int before = block_scan<THREADS>(sum, wave_sums, total);
+    if (before < want && before + sum >= want) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            if (before < want && before + n[i] >= want) {
+                found[0] = top - i;
+                found[1] = want - before;
+                found[2] = n[i];
+            }
+            before += n[i];
+        }
+    }
+    __syncthreads();
+}
+
+// Choice among up to THREADS * 4 * QUADS slots, by a workgroup per (request, kv head), which reads every weight once, into registers.
+// The smallest kept weight is found by its first 11 bits (a histogram in LDS), then, among those that share them, by the next 11 and 10 bits;
+// as soon as they are few they are put in a list, and when they are a handful they are compared with each other.  Then every slot's bit is known: kept or not.  Counts
+// of bits in front of each word give every slot its rank, by which holes and the slots that fill them find each other in a list.
+// What bounds it: the chain of steps, about 3 us of it three trips to memory, where there are few workgroups.
+template <int THREADS, int QUADS>
+__global__ __launch_bounds__(THREADS) void select_kernel(const int32_t *ctx, const int32_t *bt, const float *weights, int max_blocks, int Hkv, int max_ctx, int keep,
+                                                         int recent, int32_t *slots, int32_t *new_lens)
+{
+    constexpr int MOST = THREADS * 4 * QUADS, WORDS = MOST / 32;
+    constexpr int COPIES = THREADS > 256 ? 4 : 1;
+    static_assert(WORDS <= THREADS && MOST <= 65536, "a word to a thread, slots in 16 bits");
+    __shared__ __attribute__((aligned(16))) uint32_t hist[kDigits * COPIES];
+    __shared__ uint32_t kept[WORDS], front[WORDS];       // front: equals, then kept slots in front of the word
+    __shared__ __attribute__((aligned(16))) uint32_t candidate[kCandidates + 4];
+    __shared__ uint16_t mover[MOST / 2];                 // (there are as many holes among `heavy` slots: at most half of all)
+    __shared__ int wave_sums[THREADS / 64], found[3], candidates;
+    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x / Hkv, kh = blockIdx.x - b * Hkv;
+    const int L = min(min(max(ctx[b], 0), max_blocks * kPage), max_ctx);
+    const int n = min(L, keep), r = min(recent, n), heavy = n - r, old = L - r;
+    int32_t *to = slots + ((size_t)b * Hkv + kh) * keep;
+    if (kh == 0 && tid == 0) new_lens[b] = n;
+    if (L <= keep || heavy == 0) {
+        for (int i = tid; i < keep; i += THREADS) to[i] = i < n ? i + (L - n) : -1;
+        return;
+    }
+    const int32_t *row = bt + (size_t)b * max_blocks;
+    uint32_t u[QUADS][4];                                // 0: no old slot
+    {
+        int page[QUADS];
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q) page[q] = row[min(4 * (q * THREADS + tid), old - 1) / kPage];
+#pragma unroll
+        for (int q = 0; q < QUADS; ++q) {
+            const int j = min(4 * (q * THREADS + tid), (old - 1) & ~3);
+            const f32x4 w = *reinterpret_cast<__attribute__((address_space(1))) const f32x4 *>((uintptr_t)(weights + ((size_t)page[q] * Hkv + kh) * kPage + j % kPage));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[q][i] = 4 * (q * THREADS + tid) + i < old ? ordered(w[i]) : 0u;
+        }
+    }
+    uint32_t least = 0;                                  // the smallest kept weight, and how many of the equal ones are kept, of how many
+    int want = heavy, equal = 0;
+    bool listed = false;
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        const uint32_t digits = pass == 2 ? 1023u : 2047u;
+        // those that agree with the digits so far lie this close above `least`, whose other bits are 0 (a slot that does not count, 0, lies far off)
+        const uint32_t span = pass == 0 ? 0xffffffffu : pass == 1 ? 1u << 21 : 1u << 10;
+        clear_digits<THREADS, COPIES>(hist);
+        if (tid == 0) candidates = 0;
+        __syncthreads();
+        int zeros = 0;
+        if (listed) {
+            for (int k = tid; k < equal; k += THREADS) {
+                const uint32_t c = candidate[k];
+                count_digit<COPIES>(hist, c, shift, digits, c - least < span, zeros);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < QUADS; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) count_digit<COPIES>(hist, u[q][i], shift, digits, u[q][i] != 0 && u[q][i] - least < span, zeros);
+        }
+        count_zeros<COPIES>(hist, shift, digits, zeros);
+        __syncthreads();
+        const int in_list = equal;
+        find_digit<THREADS, COPIES>(hist, want, wave_sums, found);
+        least |= (uint32_t)found[0] << shift;
+        want = found[1];
+        equal = found[2];
+        if (want == equal || pass == 2) break;           // (all that share the digits so far are kept)
+        const uint32_t close = 1u << shift;
+        if (!listed && equal <= kCandidates) {
+            int mine = 0;
+#pragma unroll
+            for (int q = 0; q < QUADS; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mine += u[q][i] - least < close;
+            const int incl = wave_scan(mine);
+            int at = 0;
+            if (lane == 63) at = atomicAdd(&candidates, incl);
+            at = __builtin_amdgcn_readlane(at, 63) + incl - mine;
+#pragma unroll
+            for (int q = 0; q < QUADS; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (u[q][i] - least < close) candidate[at++] = u[q][i];
+        } else if (listed) {                             // (once more, only those that are left)
+            uint32_t c[kCandidates / THREADS];
+#pragma unroll
+            for (int i = 0; i < kCandidates / THREADS; ++i) c[i] = i * THREADS + tid < in_list ? candidate[i * THREADS + tid] : 0u;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kCandidates / THREADS; ++i)
+                if (c[i] - least < close) candidate[atomicAdd(&candidates, 1)] = c[i];
+        }
+        listed = listed || equal <= kCandidates;
+        if (equal <= kCompared) {
+            if (tid < 4) candidate[equal + tid] = 0;     // (no candidate is 0)
+            __syncthreads();
+            if (tid < equal) {
+                const uint32_t c = candidate[tid];
+                int above = 0, same = 0;
+                for (int i = 0; i < equal; i += 4) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(candidate + i);
+                    above += (x.x > c) + (x.y > c) + (x.z > c) + (x.w > c);
+                    same += (x.x == c) + (x.y == c) + (x.z == c) + (x.w == c);
+                }
+                if (above < want && above + same >= want) {      // (so do all that are equal to it, with the same to say)
+                    found[0] = (int)c;
+                    found[1] = want - above;
+                    found[2] = same;
+                }
+            }
+            __syncthreads();
+            least = (uint32_t)found[0];
+            want = found[1];
+            equal = found[2];
+            break;
+        }
+        __syncthreads();                                 // (found has been read, the list is whole)
+    }
+    const bool all_equals = want == equal;
+    // a bit for every old slot: kept, or equal to the smallest kept weight.  (Where all that share its first digits are kept, the others of its
+    // bits are 0.)
+#pragma unroll
+    for (int q = 0; q < QUADS; ++q) {
+        uint32_t more = 0, same = 0;
+        if (all_equals) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) more |= (uint32_t)(u[q][i] >= least) << i;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                more |= (uint32_t)(u[q][i] > least) << i;
+                same |= (uint32_t)(u[q][i] == least) << i;
+            }
+            same = or_eight(same << 4 * (tid & 7));
+        }
+        more = or_eight(more << 4 * (tid & 7));
+        if ((tid & 7) == 0) {
+            kept[(q * THREADS + tid) / 8] = more;
+            front[(q * THREADS + tid) / 8] = same;
+        }
+    }
+    __syncthreads();
+    uint32_t mine = tid < WORDS ? kept[tid] : 0u;
+    int total;
+    if (!all_equals) {                                   // the first `want` of the equals
+        uint32_t same = tid < WORDS ? front[tid] : 0u;
+        for (int at = block_scan<THREADS>(__popc(same), wave_sums, total); same != 0 && at < want; same &= same - 1, ++at) mine |= same & -same;
+        if (tid < WORDS) kept[tid] = mine;
+    }
+    const int before = block_scan<THREADS>(__popc(mine), wave_sums, total);
+    if (tid < WORDS) front[tid] = before;
+    __syncthreads();
+    auto kept_before = [&](int j) -> int {               // (j < MOST)
+        return front[j / 32] + __popc(kept[j / 32] & ((1u << (j % 32)) - 1u));
+    };
+    const int stay = kept_before(heavy);                 // (heavy < old)
+    if (tid < WORDS) {                                   // the kept slots from `heavy` on, in order
+        int at = before;
+        uint32_t x = mine;
+        if (32 * tid < heavy) {
+            const uint32_t low = heavy - 32 * tid >= 32 ? ~0u : (1u << (heavy - 32 * tid)) - 1u;
+            at += __popc(x & low);
+            x &= ~low;
+        }
+        for (; x != 0; x &= x - 1, ++at) mover[at - stay] = (uint16_t)(32 * tid + __builtin_ctz(x));
+    }
+    __syncthreads();
+    for (int i = tid; i < keep; i += THREADS) {
+        int src = i < n ? i + (L - n) : -1;
+        if (i < heavy) src = kept[i / 32] >> (i % 32) & 1 ? i : (int)mover[i - kept_before(i)];
+        to[i] = src;
+    }
+}
+
+// The same among any number of slots: the weights are read again for every digit.
+constexpr int kSelectThreads = 1024;
+
+__global__ __launch_bounds__(kSelectThreads) void select_many_kernel(SelectParams p)
 {
     extern __shared__ uint32_t smem[];
     __shared__ int wave_sums[kSelectThreads / 64];
@@ -73,30 +316,22 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
     uint32_t prefix = 0;
     int want = heavy;                                    // so many of those that agree with the prefix
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 0 ? 32 : pass == 1 ? 21 : 10;
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above = pass == 1 ? 21 : 10;
         const uint32_t mask = pass == 2 ? 1023 : 2047;
         for (int i = tid; i < kDigits; i += kSelectThreads) hist[i] = 0;
         __syncthreads();
+        int zeros = 0;
         for (int j = 4 * tid; j < old; j += 4 * kSelectThreads) {
             const f32x4 w = load4(j);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t u = ordered(w[i]);
-                if (j + i < old && (pass == 0 || (u >> above) == (prefix >> above))) atomicAdd(&hist[(u >> shift) & mask], 1u);
+                count_digit<1>(hist, u, shift, mask, j + i < old && (pass == 0 || ((u ^ prefix) >> above) == 0), zeros);
             }
         }
+        count_zeros<1>(hist, shift, mask, zeros);
         __syncthreads();
-        // from the largest digit down: thread i has digits 2047 - 2i and 2046 - 2i
-        const int hi = hist[kDigits - 1 - 2 * tid], lo = hist[kDigits - 2 - 2 * tid];
-        int total;
-        const int before = block_scan(hi + lo, wave_sums, total);
-        if (before < want && before + hi + lo >= want) {
-            const bool first = before + hi >= want;
-            found[0] = kDigits - 1 - 2 * tid - (first ? 0 : 1);
-            found[1] = want - before - (first ? 0 : hi);
-            found[2] = first ? hi : lo;
-        }
-        __syncthreads();
+        find_digit<kSelectThreads, 1>(hist, want, wave_sums, found);
         prefix |= (uint32_t)found[0] << shift;
         want = found[1];
     }
@@ -116,13 +351,8 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
                 }
             }
         }
-        more <<= 4 * (tid & 7);
-        equal <<= 4 * (tid & 7);
-#pragma unroll
-        for (int d = 1; d < 8; d <<= 1) {
-            more |= __shfl_xor(more, d);
-            equal |= __shfl_xor(equal, d);
-        }
+        more = or_eight(more << 4 * (tid & 7));
+        equal = or_eight(equal << 4 * (tid & 7));
         if ((tid & 7) == 0 && j < words * 32) {
             kept[j / 32] = more;
             other[j / 32] = equal;
@@ -135,13 +365,13 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(SelectParams p)
         // the first `want` of the equals
         int mine = 0;
         for (int w = w0; w < w1; ++w) mine += __popc(other[w]);
-        int at = block_scan(mine, wave_sums, total);
+        int at = block_scan<kSelectThreads>(mine, wave_sums, total);
         for (int w = w0; w < w1; ++w)
             for (uint32_t x = other[w]; x != 0 && at < want; x &= x - 1, ++at) kept[w] |= x & -x;
     }
     int mine = 0;
     for (int w = w0; w < w1; ++w) mine += __popc(kept[w]);
-    int at = block_scan(mine, wave_sums, total);
+    int at = block_scan<kSelectThreads>(mine, wave_sums, total);
     for (int w = w0; w < w1; ++w) {
         other[w] = at;                                   // kept slots in front of the word
         at += __popc(kept[w]);
@@ -315,12 +545,24 @@ static size_t select_lds(int32_t max_ctx) { return ((size_t)kDigits + 2 * ((size
 
 hipError_t tetri_launch_select(const SelectParams &p, hipStream_t stream)
 {
+    const dim3 grid((unsigned)(p.B * p.Hkv));
+    if (p.max_ctx <= 32768) {
+        // as many threads as give each 8 to 32 weights: 64 requests of up to 2048 tokens, 40 heads, 2560 workgroups of 256 threads
+        const auto launch = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, p.ctx, p.bt, p.weights, p.max_blocks, p.Hkv, p.max_ctx, p.keep, p.recent, p.slots, p.new_lens);
+        };
+        if (p.max_ctx <= 2048) launch(select_kernel<256, 2>, 256);
+        else if (p.max_ctx <= 8192) launch(select_kernel<512, 4>, 512);
+        else if (p.max_ctx <= 16384) launch(select_kernel<1024, 4>, 1024);
+        else launch(select_kernel<1024, 8>, 1024);
+        return hipGetLastError();
+    }
     const size_t lds = select_lds(p.max_ctx);
     if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(select_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(select_many_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(select_kernel, dim3((unsigned)(p.B * p.Hkv)), dim3(kSelectThreads), lds, stream, p);
+    hipLaunchKernelGGL(select_many_kernel, grid, dim3(kSelectThreads), lds, stream, p);
     return hipGetLastError();
 }
 
