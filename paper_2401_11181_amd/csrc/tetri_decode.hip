@@ -141,6 +141,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
     __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
     __shared__ float stat[NW][W ? 3 : 2][32];
     __shared__ int arrived;
+    __shared__ float log_sum[W ? 32 : 1];
     // (the structure lies behind the leading arguments)
     const const_decode_args *p = (const const_decode_args *)((__attribute__((address_space(4))) const char *)__builtin_amdgcn_kernarg_segment_ptr() + kDecodeLead);
 
@@ -276,6 +277,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
     // ---- the first loads.  c*: the current step, n*: the one after it (FP8: in flight as well)
     settle();
     int cb = fj.b, cs = fs, cL = fj.L;
+    [[maybe_unused]] int warm = 0;                       // W: steps behind this one, two at most
     [[maybe_unused]] int nb = 0, ns = -1, nL = 0;
     if (cs >= 0) {
         issue(false, 0);
@@ -330,12 +332,14 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
     while (cs >= 0 && (!RANGES || cb == job.b)) {
         const bool far = fs >= 0, last = cs + 1 == (cL + 32) >> 5;      // loads to issue; the request's last step
         const int new_row = cL - cs * 32;                               // (the new token's place in the last step)
-        // K has landed when only what was issued after it is outstanding
+        // K has landed when only what was issued after it is outstanding (W: also the four stores of each step that has been made since)
         if constexpr (FP8) {
-            if (ns >= 0) wait_vm<3 * NI>();
+            if (W && warm >= 2 && ns >= 0) wait_vm<3 * NI + 8>();
+            else if (ns >= 0) wait_vm<3 * NI>();
             else wait_vm<NI>();
         } else {
-            wait_vm<NI>();
+            if (W && warm >= 1) wait_vm<NI + 4>();
+            else wait_vm<NI>();
         }
         asm volatile("" : "+v"(kbase0), "+v"(vbase0));
         const char *tiles = my + buf;
@@ -361,18 +365,6 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
 #pragma unroll
             for (int v = 0; v < 16; ++v)
                 if (key_of(v) > new_row - (FP8 ? 1 : 0)) sc[v] = masked;
-        }
-        if constexpr (W) {
-            // four or eight neighbouring keys of a query head to a lane.  (A step past the row's end: a context longer than the caller said)
-            const int stride = p->score_stride;
-            if (cs * 32 < stride && l32 < p->g) {
-                float *row = p->scores + ((size_t)cb * p->Hq + (size_t)kh * p->g + l32) * stride + cs * 32;
-#pragma unroll
-                for (int v = 0; v < 16; v += 4) {
-                    const f32x4 t = {sc[v] * c, sc[v + 1] * c, sc[v + 2] * c, sc[v + 3] * c};
-                    *reinterpret_cast<__attribute__((address_space(1))) f32x4 *>((uintptr_t)(row + key_of(v))) = t;
-                }
-            }
         }
         bf16x8 pf[2];
         [[maybe_unused]] float unrounded = 0.f;
@@ -418,13 +410,16 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
         if constexpr (W) lfull += unrounded;
         // V has landed when only what was issued after it is outstanding
         if constexpr (FP8) {
-            if (far) wait_vm<3 * NI>();
+            if (W && warm >= 2 && far) wait_vm<3 * NI + 8>();
+            else if (far) wait_vm<3 * NI>();
             else if (ns >= 0) wait_vm<2 * NI>();
             else wait_vm<0>();
         } else {
-            if (far) wait_vm<NI>();
+            if (W && warm >= 1 && far) wait_vm<NI + 4>();
+            else if (far) wait_vm<NI>();
             else wait_vm<0>();
         }
+        if constexpr (W) warm = min(warm + 1, 2);
         bf16x8 vf[2 * DBLK];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -442,6 +437,18 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (far) issue(true, buf);
+        if constexpr (W) {
+            // four or eight neighbouring keys of a query head to a lane, behind the loads that the next step waits for; through the L2, where they
+            // only take room, and because another workgroup may read them.  (A step past the row's end, of a context longer than the
+            // caller said: no weight of that request is added, whatever stands here; a step's four stores are counted on.)
+            if (l32 < p->g) {
+                const int stride = p->score_stride;
+                float *row = p->scores + ((size_t)cb * p->Hq + (size_t)kh * p->g + l32) * stride + min(cs * 32, stride - 32);
+#pragma unroll
+                for (int v = 0; v < 16; v += 4)
+                    store_coherent(reinterpret_cast<f32x4 *>(row + key_of(v)), f32x4{sc[v] * c, sc[v + 1] * c, sc[v + 2] * c, sc[v + 3] * c});
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -473,8 +480,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                 lsum = lsum * alpha + (half == 0 ? (float)wgt : 0.f);
                 if constexpr (W) {
                     lfull = lfull * alpha + (half == 0 ? __builtin_amdgcn_exp2f(score - m) : 0.f);
-                    if (lane < p->g)
-                        *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(p->new_scores + (size_t)cb * p->Hq + (size_t)kh * p->g + lane)) = score;
+                    if (lane < p->g) store_coherent(p->new_scores + (size_t)cb * p->Hq + (size_t)kh * p->g + lane, score);
                 }
                 bf16x8 pn = __builtin_bit_cast(bf16x8, none);
                 if (half == 0) pn[0] = (__bf16)((float)wgt * p->v_inv);
@@ -570,7 +576,10 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
         *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)(out + at)) = __builtin_bit_cast(uint32_t, r);
     };
     auto write_lse = [&](int col, float ref, float sum) {
-        if constexpr (W) *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(e->lse + head + col)) = ref + __builtin_amdgcn_logf(sum);
+        if constexpr (W) {
+            log_sum[col] = ref + __builtin_amdgcn_logf(sum);
+            *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(e->lse + head + col)) = log_sum[col];
+        }
     };
     for (int c0 = 0; c0 < g; c0 += kMergeCols) {
         if (c0 != 0) lds_barrier();                      // everybody is done with the columns before
@@ -623,6 +632,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             }
         }
     }
+    bool finished = whole;
     if (!whole) {
         coherent_stores_done();
         lds_barrier();
@@ -632,6 +642,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             // all the others have been here: the counter goes back to zero, the parts are merged in their order.  With few
             // columns the threads form groups that take every groups-th part, and the groups meet in LDS.
             if (te == 0) store_global(e->counters + counter, 0);
+            finished = true;
             if constexpr (W) {
                 if (te < g) {
                     float ref = -INFINITY, sum = 0.f;
@@ -701,6 +712,47 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                 }
                 if (on && grp == 0) write_pair(head * D + 2 * v, x, y, l);
             }
+        }
+    }
+    if constexpr (W) {
+        if (e->weights_w != nullptr && finished) {
+            // the request is done with: its weights, four neighbouring keys to a lane.  (The scores of this workgroup's wavefronts and of the others
+            // have been performed: each waited for its own before it arrived.)
+            if (whole) coherent_stores_done();
+            lds_barrier();
+            const int32_t *table = bt + (size_t)job.b * max_blocks;
+            const int stride = e->score_stride, append = e->pages_w != nullptr ? 1 : 0;
+            const float *scores = e->scores + head * stride;
+            typedef __attribute__((address_space(1))) f32x4 global_f32x4;
+            if (job.L < stride)
+                for (int j = 4 * te; j < job.L + append; j += 4 * NT) {
+                    float *at = e->weights_w + ((size_t)table[j / kPage] * Hkv + kh) * kPage + j % kPage;
+                    f32x4 x = *reinterpret_cast<global_f32x4 *>((uintptr_t)at);
+                    if (job.L - j < 4) {                 // (the new token's slot holds nothing yet)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (j + i == job.L) x[i] = 0.f;
+                    }
+                    for (int h = 0; h < g; ++h) {
+                        const float2 lo = load_coherent2(scores + (size_t)h * stride + j), hi = load_coherent2(scores + (size_t)h * stride + j + 2);
+                        const float t[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float s = t[i];
+                            if constexpr (FP8) {
+                                if (j + i == job.L) s = load_coherent(e->new_scores + head + h);
+                            }
+                            x[i] += __builtin_amdgcn_exp2f(s - log_sum[h]);
+                        }
+                    }
+                    if (j + 4 <= job.L + append) {
+                        *reinterpret_cast<global_f32x4 *>((uintptr_t)at) = x;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 3; ++i)
+                            if (j + i < job.L + append) *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(at + i)) = x[i];
+                    }
+                }
         }
     }
     if (!RANGES || left == 0) break;

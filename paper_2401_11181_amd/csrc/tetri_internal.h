@@ -288,6 +288,7 @@ struct DecodeWeightArgs : DecodeArgs {
     float *scores;        // [request][query head][score_stride]: every cached key's score, times scale and log2(e)
     float *new_scores;    // [request][query head]: the new token's
     float *lse;           // [request][query head]: log2 of the softmax's sum of exponentials
+    float *weights_w;     // the slots' weights, added to by the launch itself (null: by another one)
     int32_t score_stride; // a multiple of 32
 };
 
@@ -305,7 +306,7 @@ struct DecodeParams : DecodeWeightArgs {
 
 // What a decode iteration that gives its weights needs besides the arguments of the others (host).
 struct DecodeWeights {
-    float *scores, *new_scores, *lse;
+    float *scores, *new_scores, *lse, *weights_w;
     int32_t score_stride;
 };
 
