@@ -156,6 +156,8 @@ WEIGH = {
     "ragged": ([(5, 33), (40, 0), (1, 700), (30, 15), (17, 16)], 100, 6, 2, 128),
     "gqa8": ([(100, 300), (28, 1)], 128, 8, 1, 64),
     "gqa32": ([(9, 40)], 16, 32, 1, 128),
+    "gqa5": ([(33, 70), (20, 0)], 64, 10, 2, 64),
+    "gqa40": ([(21, 50)], 32, 40, 1, 64),
     "long": ([(200, 2500), (56, 130)], 300, 4, 4, 128),
 }
 
@@ -215,6 +217,43 @@ def test_weigh_many_segments():
     run_weigh([(1 + i % 3, (37 * i) % 90) for i in range(90)], 200, 2, 1, 64, 2, 97, False)
 
 
+@pytest.mark.parametrize("hq,hkv,d,n,L,last,fp8", [
+    (32, 16, 64, 300, 8000, 300, False),          # hundreds of rows a kv head, 64 keys to a wavefront
+    (16, 16, 128, 700, 7700, 700, True),
+    (8, 2, 128, 40, 9000, 16, False),             # few rows, keys in many parts
+    (4, 4, 128, 513, 0, 2000, False),             # no context
+])
+def test_weigh_large(hq, hkv, d, n, L, last, fp8):
+    """Against torch in 64 bits, on the GPU."""
+    c = ec.Cache([L], hkv, d, 99, fp8, room=n)
+    gen = torch.Generator().manual_seed(100)
+    q, k = (torch.randn((n, heads, d), generator=gen).to(torch.bfloat16).to(DEV) for heads in (hq, hkv))
+    h = handle(c, hq, n, 1)
+    weights = dev(torch.nan_to_num(c.weights))
+    want = weights.double()
+    work = workspace(h.tetri_chunk_prefill_weights_workspace(1, L, last))
+    h.tetri_chunk_prefill_weights(q, k, dev(c.pool), weights, dev(c.bt), dev(np.array([0, n], dtype=np.int32)), dev(c.ctx), 1, L, last, d ** -0.5,
+                                  int(fp8), ec.K_SCALE, work, work.numel())
+    pages, places = (dev(x.astype(np.int64)) for x in c.slots(0, L + n))
+    pool = torch.from_numpy(c.float_pool()).to(DEV)
+    rows = min(n, last)
+    t = torch.arange(n - rows, n, device=DEV)
+    hidden = torch.arange(L + n, device=DEV)[None] > (L + t)[:, None]
+    want[pages[L:], :, places[L:]] = 0.0
+    before, amp = want.clone(), 0.0
+    for kh in range(hkv):
+        keys = torch.cat([pool[pages[:L], 0, kh, places[:L]], k[:, kh].double()])
+        for head in range(kh * hq // hkv, (kh + 1) * hq // hkv):
+            x = q[n - rows:, head].double()
+            want[pages, kh, places] += torch.softmax((x @ keys.T * d ** -0.5).masked_fill(hidden, float("-inf")), 1).sum(0)
+            amp = max(amp, float((x.abs() @ keys.abs().T).max()) * d ** -0.5)
+    want, before = want.cpu().numpy(), before.cpu().numpy()
+    bound = ec.weight_bound(want - before, before, amp, d)
+    off = np.abs(weights.cpu().double().numpy() - want)
+    assert (off <= bound).all(), float((off / bound).max())
+    h.close()
+
+
 def test_weigh_large_scores():
     """Scores of some hundreds: one key takes nearly all of a row's weight, and the largest lies anywhere."""
     run_weigh([(64, 400)], 64, 2, 2, 128, 1000, 98, False, std=6.0)
@@ -265,7 +304,7 @@ def test_select(kind, keep, recent):
     run_select(c, keep, recent, pad=(keep * 7) % 50)
 
 
-@pytest.mark.parametrize("length", [4096, 4097, 40000])
+@pytest.mark.parametrize("length", [2048, 2049, 4097, 8193, 16384, 16385, 32768, 32769, 40000])
 def test_select_long(length):
     c = ec.Cache([length, 9], 1, 64, 122)
     for kind in ("spread", "few"):
@@ -431,6 +470,34 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert torch.equal(w.view(torch.uint8), want[1].view(torch.uint8))
     h.close()
+
+
+def test_far_pages():
+    """Pages behind more than 4 GB of pool and of codes, and what the same request gives in a small pool."""
+    hq, hkv, d, keep, recent = 16, 8, 128, 40, 10
+    c = ec.Cache([90], hkv, d, 173, room=1)
+    got = []
+    for pages in (c.pages, 140000):
+        bt = np.where(c.bt < c.pages, c.bt + pages - c.pages, c.bt)
+        h = tetri.Tetri(hq, hkv, d, 64, pages, c.blocks, 8)
+        pool, w = torch.empty((pages, 2, hkv, 16, d), dtype=torch.bfloat16, device=DEV), torch.empty((pages, hkv, 16), device=DEV)
+        pool[pages - c.pages:], w[pages - c.pages:] = dev(c.pool), dev(c.weights)
+        gen = torch.Generator().manual_seed(174)
+        q, k, v = (torch.randn((1, n, d), generator=gen).to(torch.bfloat16).to(DEV) for n in (hq, hkv, hkv))
+        work = workspace(max(h.tetri_decode_attn_weights_workspace(1, 90), h.tetri_chunk_prefill_weights_workspace(1, 90, 1)))
+        out, slots = torch.zeros_like(q), torch.zeros((1, hkv, keep), dtype=torch.int32, device=DEV)
+        lens, ctx, table = torch.zeros(1, dtype=torch.int32, device=DEV), dev(c.ctx), dev(bt)
+        cq, ck = torch.zeros((64, hq, d), dtype=torch.bfloat16, device=DEV), torch.zeros((64, hkv, d), dtype=torch.bfloat16, device=DEV)
+        cq[:1], ck[:1] = q, k
+        h.tetri_chunk_prefill_weights(cq, ck, pool, w, table, dev(np.array([0, 1], dtype=np.int32)), ctx, 1, 90, 1, 0.09, 0, 1.0, work, work.numel())
+        h.tetri_decode_attn_weights(q, k, v, pool, w, table, ctx, 1, 90, 0.09, 1, 0, 1.0, 1.0, work, work.numel(), out)
+        h.tetri_kv_select(w, table, ctx, 1, 90, keep, recent, slots, lens)
+        h.tetri_kv_compact(slots, table, ctx, 1, keep, recent, pool, w, 0)
+        used = slice(pages - c.pages, pages)
+        got.append([x.cpu() for x in (pool[used], w[used], out, slots, lens)])
+        h.close()
+    for a, b in zip(*got):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
 
 
 def test_another_stream():
