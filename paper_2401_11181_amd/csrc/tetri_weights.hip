@@ -182,13 +182,23 @@ template <int D, bool CODES> __device__ __forceinline__ uint32_t tile_base(int l
     return row * StreamTile<D, CODES>::RB + (CODES ? (swz << 4) + 8 * half : (half ^ swz) << 4);
 }
 
+// Bit v: element v of a block of scores, row 8 * (v / 4) + v % 4 (and 4 * half, which the caller takes off), lies in front of row `end`.
+// (As bits, for comparisons of which one follows from another become a chain of selections.)
+__device__ __forceinline__ uint32_t rows_below(int end)
+{
+    const int e = min(max(end, 0), 32);
+    uint32_t bits = (1u << (e / 8 * 4 + min(e % 8, 4))) - 1u;
+    asm volatile("" : "+v"(bits));
+    return bits;
+}
+
 // 16 bytes per lane from base + off to LDS (see dma16; base is wave-uniform).
 __device__ __forceinline__ void dma16_at(const void *base, uint32_t off, uint32_t lds)
 {
     dma16(reinterpret_cast<const char *>(uniform_ptr(base)) + off, lds);
 }
 
-// Fragments are in their registers from here on.  (Without this the compiler waits for them where they are used, in the loop, and there every
+// Fragments are in their registers from here on.  (Without this the compiler waits for them where they are used, in the loop, and there for every
 // load to LDS that is in flight with them.)
 template <int KSTEPS> __device__ __forceinline__ void loaded(bf16x8 (&f)[KSTEPS])
 {
@@ -250,13 +260,32 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, c
     if (!find_segment(Lookup{cu, ctx, S, C, max_tokens, max_ctx, last, g}, rest / parts, lane,
                       [&](int n, int) { return (min(n, last) * g + 32 * kSub * RW - 1) / (32 * kSub * RW); }, x)) return;
     const int row0 = (x.local * RW + rw) * 32 * kSub;    // the wavefront's first row
+    // the wavefront's rows come through its part of the ring
     bf16x8 qf[kSub][KSTEPS];
     int t[kSub];                                         // the lane's rows see new keys 0..t
 #pragma unroll
-    for (int i = 0; i < kSub; ++i) {
-        const int r = min(row0 + 32 * i + l32, x.rows - 1);
-        t[i] = x.t0 + magic_div(r, p.g_magic);
-        load_rows<D>(reinterpret_cast<const char *>(p.q + query_row(p, x, kh, r) * D), half, qf[i]);
+    for (int i = 0; i < kSub; ++i) t[i] = x.t0 + magic_div(min(row0 + 32 * i + l32, x.rows - 1), p.g_magic);
+    {
+        typedef StreamTile<D, false> T;
+        constexpr int AT_ONCE = KW == 1 ? 1 : kSub;      // blocks of 32 rows
+        char *mine = smem + wave * (AT_ONCE * kStreamBytes);
+#pragma unroll
+        for (int b0 = 0; b0 < kSub; b0 += AT_ONCE) {
+#pragma unroll
+            for (int b = 0; b < AT_ONCE; ++b)
+#pragma unroll
+                for (int i = 0; i < T::NI; ++i) {
+                    const int r = T::RPI * i + lane / T::CH;
+                    const size_t row = query_row(p, x, kh, min(row0 + 32 * (b0 + b) + r, x.rows - 1));
+                    dma16(reinterpret_cast<const char *>(p.q + row * D) + (((lane % T::CH) ^ T::swizzle(r)) << 4), lds_address(mine) + b * kStreamBytes + i * 1024);
+                }
+            wait_vm<0>();
+#pragma unroll
+            for (int b = 0; b < AT_ONCE; ++b) {
+                read_tile<D, false>(mine + b * kStreamBytes, tile_base<D, false>(lane), qf[b0 + b]);
+                loaded(qf[b0 + b]);
+            }
+        }
     }
     const int t_first = __builtin_amdgcn_readfirstlane(x.t0 + magic_div(min(row0, x.rows - 1), p.g_magic));
     const int t_last = __builtin_amdgcn_readfirstlane(x.t0 + magic_div(min((x.local + 1) * RW * 32 * kSub, x.rows) - 1, p.g_magic));    // of the workgroup
@@ -264,8 +293,6 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, c
     const int each = (tiles + p.parts - 1) / p.parts, begin = min(tiles, part * each), end = min(tiles, begin + each);
     float m[kSub], l[kSub];
     const const_i32 *table = (const const_i32 *)(uintptr_t)(p.bt + (size_t)x.s * p.max_blocks);
-#pragma unroll
-    for (int i = 0; i < kSub; ++i) loaded(qf[i]);
     char *ring = smem + kw * (DEPTH * kStreamBytes);
     const uint32_t ring_lds = lds_address(ring);
 
@@ -338,9 +365,10 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, c
         auto mask = [&](int it, int b) {
             if (it == partial || it >= mask_from) {
                 const int most = it >= to ? -1 : it < old_tiles ? x.L - 1 - 32 * it - 4 * half : t[b] - 32 * (it - old_tiles) - 4 * half;
+                const uint32_t seen = rows_below(most + 1);
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    if (8 * (v / 4) + v % 4 > most) sc[b][v] = none;
+                    if (!(seen & 1u << v)) sc[b][v] = none;
             }
         };
         lds_barrier();                                   // (the ring's last tiles have been read)
@@ -442,7 +470,8 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float2 *stats, fl
     if (threadIdx.x % 16 == 0) lse[row] = m + __builtin_amdgcn_logf(l);
 }
 
-// Second pass: the weights.  A wavefront keeps 32 * SUB keys of one kv head and the workgroup goes over the query rows that see any of its
+// Second pass: the weights.  (The keys' fragments come straight from memory, beside the first tiles of rows: by way of LDS, in full cache lines, they
+// were a trip of their own, and 16896 keys of 8 kv heads took 26 us instead of 18.)  A wavefront keeps 32 * SUB keys of one kv head and the workgroup goes over the query rows that see any of its
 // 128 * SUB; S = Q K^T: a lane has a key.  64 keys to a wavefront halve what is read from LDS; 32 where that leaves compute units without
 // work.
 template <int D, bool FP8, int SUB>
@@ -503,10 +532,10 @@ __global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const
         const int all_see = cached ? 0 : (key0 + 32 * SUB - 1 - x.t0) * g;
         auto mask = [&](int rt, int b, f32x16 &s) {
             if (rt * 32 < all_see) {
-                const int least = first_row[b] - rt * 32 - 4 * half;
+                const uint32_t blind = rows_below(first_row[b] - rt * 32 - 4 * half);
 #pragma unroll
                 for (int v = 0; v < 16; ++v)
-                    if (8 * (v / 4) + v % 4 < least) s[v] = none;
+                    if (blind & 1u << v) s[v] = none;
             }
         };
         lds_barrier();                                   // (everybody is done with the item before)
