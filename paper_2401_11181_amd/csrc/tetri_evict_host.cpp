@@ -65,22 +65,24 @@ int64_t decode_bytes(const tetri_ctx *h, int32_t num_reqs, int32_t max_ctx_len)
     return (int64_t)num_reqs * h->cfg.num_q_heads * (score_stride(max_ctx_len) + 2) * 4;
 }
 
-// How the first pass of weighing a chunk is cut.  Wavefronts of a workgroup that have rows of their own share the keys they read; with as
-// many as a segment's rows fill, on average.  The keys of a row tile are cut in as many parts as give every compute unit two
-// workgroups, none of fewer than eight tiles of keys.
+// How the first pass of weighing a chunk is cut.  Wavefronts of a workgroup that have rows of their own share the keys they read: as many as a
+// segment's rows fill, on average, and not so many that workgroups are lacking.  The keys of a row tile are cut in as many parts as
+// give every compute unit two workgroups, none of fewer than eight tiles of keys.  (40 heads, 512 rows, no context: 22 us with wavefronts of
+// one's own, 27 with four that share; 256 rows behind 8000 tokens: 87 and 80.)
 struct WeighShape {
     int32_t row_waves, parts;
 };
 WeighShape weigh_shape(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
 {
     const int64_t g = h->cfg.num_q_heads / h->cfg.num_kv_heads, rows = std::min<int64_t>(h->cfg.chunk_size, (int64_t)num_segs * last_rows) * g;
-    const int64_t mean = rows / num_segs;
-    WeighShape w;
-    w.row_waves = mean >= 512 ? 4 : mean > 64 ? 2 : 1;
-    const int64_t tile = 64 * w.row_waves, wgs = (rows + tile - 1) / tile * h->cfg.num_kv_heads;
+    const int64_t mean = rows / num_segs, places = 2 * std::max(h->num_cus, 1);
     const int64_t tiles = ((int64_t)max_ctx_len + std::min(h->cfg.chunk_size, last_rows)) / 32 + 2;
-    w.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({2 * std::max(h->num_cus, 1) / wgs, tiles / 8, kWeighParts}));
-    return w;
+    WeighShape w;
+    for (w.row_waves = mean >= 512 ? 4 : mean > 64 ? 2 : 1;; w.row_waves /= 2) {
+        const int64_t tile = 64 * w.row_waves, wgs = (rows + tile - 1) / tile * h->cfg.num_kv_heads;
+        w.parts = (int32_t)std::max<int64_t>(1, std::min<int64_t>({places / wgs, tiles / 8, kWeighParts}));
+        if (w.row_waves == 1 || wgs * w.parts >= places * 3 / 4) return w;
+    }
 }
 
 int64_t weigh_bytes(const tetri_ctx *h, int32_t num_segs, int32_t max_ctx_len, int32_t last_rows)
