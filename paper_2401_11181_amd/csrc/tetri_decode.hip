@@ -724,7 +724,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             const int stride = e->score_stride, append = e->pages_w != nullptr ? 1 : 0;
             const float *scores = e->scores + head * stride;
             typedef __attribute__((address_space(1))) f32x4 global_f32x4;
-            if (job.L < stride)
+            if (job.L < stride && job.L + append <= max_blocks * kPage)      // (not longer than the caller said)
                 for (int j = 4 * te; j < job.L + append; j += 4 * NT) {
                     float *at = e->weights_w + ((size_t)table[j / kPage] * Hkv + kh) * kPage + j % kPage;
                     f32x4 x = *reinterpret_cast<global_f32x4 *>((uintptr_t)at);

@@ -244,7 +244,7 @@ __device__ __forceinline__ size_t query_row(const WeighParams &p, const Segment 
 
 // First pass: reference exponent and sum of the softmax of every row over a part of its keys.  RW wavefronts share a stream of key tiles,
 // each with 64 rows of its own; the 4 / RW streams of a workgroup take the tiles of the part in turn.  S^T = K Q^T: a lane has a
-// row.  The reference is the largest score of the row's first tile and stays so as long as the sum does not overflow: in fp32 a large
+// row.  The reference is the largest score of the row's first tile and stays so as long as the sum is below 2^100: in fp32 a large
 // sum is as exact as a small one.
 template <int D, bool FP8, int RW>
 __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, const int32_t *ctx, int S, int C, int max_tokens, int max_ctx, int last, int g,
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, c
         rescue(1, c, before);
         wait_vm<0>();
     };
-    // The reference is looked at in a row's first tile and then only if the sum has overflowed: once more with a look at every tile.  (All
+    // The reference is looked at in a row's first tile and then only if the sum has got too large: once more with a look at every tile.  (All
     // wavefronts of the workgroup go along, for the barriers.)
     __shared__ int overflow;
     if (tid == 0) overflow = 0;
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(256, 2) void weigh_rows_kernel(const int32_t *cu, c
             stream(std::false_type(), careful, begin, end);
         }
         if (careful) break;
-        if (__builtin_amdgcn_ballot_w64(!(l[0] < INFINITY) || !(l[1] < INFINITY))) overflow = 1;
+        if (__builtin_amdgcn_ballot_w64(!(l[0] <= 0x1p100f) || !(l[1] <= 0x1p100f))) overflow = 1;     // (sums of these do not overflow either)
         __syncthreads();
         if (!overflow) break;
     }

@@ -106,6 +106,24 @@ class ChunkedPrefill:
     def attn_fp8(self, c, q, k_new, v_new, kv_pages_fp8, scale, k_scale, v_scale, append, out, stream=None):
         self._launch(c, q, k_new, v_new, kv_pages_fp8, scale, append, 1, k_scale, v_scale, out, stream)
 
+    def weights_workspace(self, c, last_rows):
+        """Bytes of device memory that weights() needs for chunk c."""
+        return self.handle.tetri_chunk_prefill_weights_workspace(self.meta[c][3], self._longest_ctx(c), last_rows)
+
+    def weights(self, c, q, k_new, kv_pages, kv_weights, scale, last_rows, workspace, k_scale=None, stream=None):
+        """Adds to kv_weights what the last rows of chunk c's segments give to the keys.  k_scale: that of a pool of FP8 codes
+        (None: a 16-bit pool)."""
+        cu, ctx, bt, S = self.meta[c]
+        self.handle.tetri_chunk_prefill_weights(q, k_new, kv_pages, kv_weights, bt, cu, ctx, S, self._longest_ctx(c), last_rows, scale,
+                                                int(k_scale is not None), 1.0 if k_scale is None else k_scale, workspace,
+                                                workspace.numel() * workspace.element_size(), stream)
+
+    def _longest_ctx(self, c):
+        # (an entry of `meta` that has been replaced may have any contexts that the block table can hold)
+        if self.meta[c] is self._planned[c] and (self._meta_version is None or self.meta_dev._version == self._meta_version):
+            return max(start for _, start, _ in self.chunk_segments(c))
+        return self.max_blocks * 16
+
     def validate(self, c):
         cu, ctx, bt, S = self.meta[c]
         self.handle.tetri_validate_chunk(bt, cu, ctx, S)

@@ -10,6 +10,7 @@ import torch
 from oracle import decode as odecode
 from oracle import evict
 from paper_2401_11181_amd import tetri
+from paper_2401_11181_amd.prefill import ChunkedPrefill
 import evict_common as ec
 import gpu_common as gc
 
@@ -146,6 +147,23 @@ def test_decode_longer_than_said():
     h.close()
 
 
+def test_decode_longer_than_said_with_append():
+    """A request that fills its block table has no slot for a new token: neither its weights nor any other's are touched for it."""
+    c = ec.Cache([80, 30], 2, 128, 64, room=[0, 50], extra_blocks=0)
+    h = handle(c, 4)
+    assert c.blocks == 5
+    bf = lambda n: torch.randn(2, n, 128, device=DEV).to(torch.bfloat16)
+    w, out = dev(c.weights.clone()), torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=DEV)
+    work = workspace(h.tetri_decode_attn_weights_workspace(2, 64))
+    h.tetri_decode_attn_weights(bf(4), bf(2), bf(2), dev(c.pool), w, dev(c.bt), dev(c.ctx), 2, 64, 0.1, 1, 0, 1.0, 1.0, work, work.numel(), out)
+    w, touched = w.cpu(), torch.zeros(c.weights.shape, dtype=torch.bool)
+    p, s = c.slots(1, 31)
+    touched[p, :, s] = True
+    assert torch.equal(w.view(torch.int32)[~touched], c.weights.view(torch.int32)[~touched])
+    assert (w[p, :, s][:30] > c.weights[p, :, s][:30]).all()
+    h.close()
+
+
 # ---------------------------------------------------------------- prefill
 
 # segments (rows, cached tokens), chunk, query heads, kv heads, head dim
@@ -254,6 +272,27 @@ def test_weigh_large(hq, hkv, d, n, L, last, fp8):
     h.close()
 
 
+def test_weigh_scores_far_above_the_first_ones():
+    """Two keys score 127.5 (as a power of two) above those before them: exp2 of that is finite, of twice it is not."""
+    c = ec.Cache([100], 1, 64, 101, room=1)
+    h = handle(c, 1, 8, 1)
+    c.pool.zero_()
+    pages, places = c.slots(0, 101)
+    for j in (64, 68):                           # (in different halves of a wavefront)
+        c.pool[pages[j], 0, 0, places[j], 0] = 8.0
+    q, k = torch.zeros((8, 1, 64), dtype=torch.bfloat16), torch.zeros((8, 1, 64), dtype=torch.bfloat16)
+    q[0, 0, 0] = 8.0
+    w = dev(torch.zeros_like(c.weights))
+    work = workspace(h.tetri_chunk_prefill_weights_workspace(1, 100, 1))
+    h.tetri_chunk_prefill_weights(dev(q), dev(k), dev(c.pool), w, dev(c.bt), dev(np.array([0, 1], dtype=np.int32)), dev(c.ctx), 1, 100, 1,
+                                  127.5 / 64 / 1.4426950408889634, 0, 1.0, work, work.numel())
+    got = w.cpu()[pages, 0, places]
+    want = torch.zeros(101)
+    want[[64, 68]] = 0.5
+    assert torch.allclose(got, want, rtol=0, atol=1e-5)
+    h.close()
+
+
 def test_weigh_large_scores():
     """Scores of some hundreds: one key takes nearly all of a row's weight, and the largest lies anywhere."""
     run_weigh([(64, 400)], 64, 2, 2, 128, 1000, 98, False, std=6.0)
@@ -267,7 +306,7 @@ def run_select(c, keep, recent, max_ctx=None, pad=0):
     slots = torch.full((B, c.hkv, keep), 77, dtype=torch.int32, device=DEV)
     lens = torch.full((B,), 77, dtype=torch.int32, device=DEV)
     w = dev(c.weights)
-    h.tetri_kv_select(w, dev(c.bt), dev(c.ctx), B, max(c.lens) + pad, keep, recent, slots, lens)
+    h.tetri_kv_select(w, dev(c.bt), dev(c.ctx), B, max_ctx or max(c.lens) + pad, keep, recent, slots, lens)
     torch.cuda.synchronize()
     assert torch.equal(w.cpu().view(torch.int32), c.weights.view(torch.int32))
     h.close()
@@ -310,6 +349,12 @@ def test_select_long(length):
     for kind in ("spread", "few"):
         fill_weights(c, kind, 123)
         run_select(c, length // 3, 100)
+
+
+def test_select_under_the_largest_bound():
+    c = ec.Cache([1000, 70], 1, 64, 124, extra_blocks=(1 << 19) // 16)
+    fill_weights(c, "spread", 125)
+    run_select(c, 300, 20, max_ctx=1 << 19)
 
 
 # ---------------------------------------------------------------- compact
@@ -424,6 +469,34 @@ def test_prefill_decode_evict_decode(fp8):
             assert np.array_equal(got_pool[pages, :, :, places], want_pool[pages, :, :, places])
         assert have == [64, 64, 54] if turn == 0 else have == [64, 64, 63]
     h.close()
+
+
+def test_weights_of_a_scheduled_batch():
+    """ChunkedPrefill.weights: every chunk of a packed batch, against the oracle over the same chunks."""
+    hq, hkv, d, C, scale = 4, 2, 64, 48, 0.125
+    prompts = [70, 33, 90]
+    c = ec.Cache([0, 0, 0], hkv, d, 175, room=prompts, extra_blocks=0)
+    sess = ChunkedPrefill(prompts, None, C, hq, hkv, d, c.pages, [list(c.bt[b, :-(-n // 16)]) for b, n in enumerate(prompts)])
+    gen = torch.Generator().manual_seed(176)
+    bf = lambda n: [torch.randn((m, n, d), generator=gen).to(torch.bfloat16) for m in prompts]
+    q, k, v = bf(hq), bf(hkv), bf(hkv)
+    pool, w = dev(c.pool), dev(torch.nan_to_num(c.weights))
+    want = torch.nan_to_num(c.weights).double().numpy()
+    for chunk in range(sess.n_chunks):
+        cq, ck, cv = (sess.gather_chunk([dev(t) for t in x], chunk) for x in (q, k, v))
+        segs = sess.chunk_segments(chunk)
+        cu = np.concatenate([[0], np.cumsum([n for _, _, n in segs])])
+        c.pool = pool.cpu()
+        evict.prefill_weights(cq.cpu().double().numpy(), ck.cpu().double().numpy(), c.float_pool(), want, c.bt[[r for r, _, _ in segs]], cu,
+                              [start for _, start, _ in segs], 16, scale)
+        work = workspace(sess.weights_workspace(chunk, 16))
+        sess.weights(chunk, cq, ck, pool, w, scale, 16, work)
+        sess.append(chunk, ck, cv, pool)
+    got = w.cpu().double().numpy()
+    for b, n in enumerate(prompts):
+        pages, places = c.slots(b, n)
+        # (some hundred terms, all positive; 64 products a score: see evict_common)
+        assert np.allclose(got[pages, :, places], want[pages, :, places], rtol=1e-4, atol=1e-7)
 
 
 def test_captured_and_replayed():
