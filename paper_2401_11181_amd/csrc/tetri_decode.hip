@@ -724,8 +724,9 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             const int stride = e->score_stride, append = e->pages_w != nullptr ? 1 : 0;
             const float *scores = e->scores + head * stride;
             typedef __attribute__((address_space(1))) f32x4 global_f32x4;
-            if (job.L < stride && job.L + append <= max_blocks * kPage)      // (not longer than the caller said)
-                for (int j = 4 * te; j < job.L + append; j += 4 * NT) {
+            const int slots = job.L + append;            // (the host sees to it that max_ctx leaves a slot for the new token)
+            if (job.L <= e->max_ctx)                     // (not longer than the caller said)
+                for (int j = 4 * te; j < slots; j += 4 * NT) {
                     float *at = e->weights_w + ((size_t)table[j / kPage] * Hkv + kh) * kPage + j % kPage;
                     f32x4 x = *reinterpret_cast<global_f32x4 *>((uintptr_t)at);
                     if (job.L - j < 4) {                 // (the new token's slot holds nothing yet)
@@ -745,12 +746,12 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                             x[i] += __builtin_amdgcn_exp2f(s - log_sum[h]);
                         }
                     }
-                    if (j + 4 <= job.L + append) {
+                    if (j + 4 <= slots) {
                         *reinterpret_cast<global_f32x4 *>((uintptr_t)at) = x;
                     } else {
 #pragma unroll
                         for (int i = 0; i < 3; ++i)
-                            if (j + i < job.L + append) *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(at + i)) = x[i];
+                            if (j + i < slots) *reinterpret_cast<__attribute__((address_space(1))) float *>((uintptr_t)(at + i)) = x[i];
                     }
                 }
         }

@@ -122,6 +122,7 @@ tetri_status tetri_decode_attn_weights(tetri_ctx *h, const void *q, const void *
     const size_t heads = (size_t)num_reqs * h->cfg.num_q_heads;
     DecodeWeights w;
     w.score_stride = (int32_t)score_stride(max_ctx_len);
+    w.max_ctx = max_ctx_len;
     w.scores = static_cast<float *>(workspace);
     w.new_scores = w.scores + heads * w.score_stride;
     w.lse = w.new_scores + heads;
@@ -139,7 +140,7 @@ tetri_status tetri_decode_attn_weights(tetri_ctx *h, const void *q, const void *
     p.weights = kv_weights;
     p.bt = block_table; p.ctx = ctx_lens;
     p.B = num_reqs; p.Hq = h->cfg.num_q_heads; p.Hkv = h->cfg.num_kv_heads; p.g = p.Hq / p.Hkv;
-    p.max_blocks = h->cfg.max_blocks_per_seq; p.score_stride = w.score_stride; p.append = append;
+    p.max_blocks = h->cfg.max_blocks_per_seq; p.score_stride = w.score_stride; p.max_ctx = max_ctx_len; p.append = append;
     const hipError_t e = tetri_launch_add_weights(p, max_ctx_len, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return tetri_fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return TETRI_OK;

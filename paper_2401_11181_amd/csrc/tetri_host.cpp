@@ -395,6 +395,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     p.lse = weights ? weights->lse : nullptr;
     p.weights_w = weights ? weights->weights_w : nullptr;
     p.score_stride = weights ? weights->score_stride : 0;
+    p.max_ctx = weights ? weights->max_ctx : 0;
     hipError_t e = tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares && !static_scratch) ++h->counter_turn;

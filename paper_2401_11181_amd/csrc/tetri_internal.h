@@ -290,6 +290,7 @@ struct DecodeWeightArgs : DecodeArgs {
     float *lse;           // [request][query head]: log2 of the softmax's sum of exponentials
     float *weights_w;     // the slots' weights, added to by the launch itself (null: by another one)
     int32_t score_stride; // a multiple of 32
+    int32_t max_ctx;      // no weight of a longer request is added
 };
 
 // The launch as the host lays it out: what it adds goes to the kernel as leading scalars, but for the choice of the kernel.
@@ -307,7 +308,7 @@ struct DecodeParams : DecodeWeightArgs {
 // What a decode iteration that gives its weights needs besides the arguments of the others (host).
 struct DecodeWeights {
     float *scores, *new_scores, *lse, *weights_w;
-    int32_t score_stride;
+    int32_t score_stride, max_ctx;
 };
 
 // Adds a decode iteration's weights to those of the slots they fell on (tetri_weights.hip).
@@ -315,7 +316,7 @@ struct AddWeightsParams {
     const float *scores, *new_scores, *lse;
     float *weights;       // [page][kv head][slot]
     const int32_t *bt, *ctx;
-    int32_t B, Hq, Hkv, g, max_blocks, score_stride;
+    int32_t B, Hq, Hkv, g, max_blocks, score_stride, max_ctx;
     int32_t append;       // 1: the new token has a slot
 };
 

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256) void add_weights_kernel(AddWeightsParams p)
     const int kh = blockIdx.y;
     for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
         const int L = p.ctx[b];
-        if (L < 0 || L > p.max_blocks * kPage || L >= p.score_stride) continue;      // (longer than the caller said)
+        if (L < 0 || L > p.max_ctx) continue;            // (longer than the caller said)
         const int j = blockIdx.x * kAddKeys + threadIdx.x * 4;
         const size_t head = (size_t)b * p.Hq + (size_t)kh * p.g;
         if (j < L) {

@@ -164,6 +164,27 @@ def test_decode_longer_than_said_with_append():
     h.close()
 
 
+@pytest.mark.parametrize("max_ctx,others", [(61, 1), (8193, 1), (1000, 300)])
+@pytest.mark.parametrize("append", [0, 1])
+def test_decode_a_little_longer_than_said(max_ctx, others, append):
+    """One token too many is too many: no weight of that request is added; the longest that are allowed get theirs."""
+    lens = [max_ctx + 1] + [max_ctx] + [5] * (others - 1)
+    c = ec.Cache(lens, 2, 64, 65, room=[1] * len(lens))
+    h = handle(c, 4)
+    bf = lambda n: torch.randn(len(lens), n, 64, device=DEV).to(torch.bfloat16)
+    w, out = dev(c.weights.clone()), torch.zeros(len(lens), 4, 64, dtype=torch.bfloat16, device=DEV)
+    work = workspace(h.tetri_decode_attn_weights_workspace(len(lens), max_ctx))
+    h.tetri_decode_attn_weights(bf(4), bf(2), bf(2), dev(c.pool), w, dev(c.bt), dev(c.ctx), len(lens), max_ctx, 0.1, append, 0, 1.0, 1.0, work,
+                                work.numel(), out)
+    w = w.cpu()
+    p, s = c.slots(0, max_ctx + 1 + append)
+    assert torch.equal(w[p, :, s].view(torch.int32), c.weights[p, :, s].view(torch.int32))
+    for b in range(1, len(lens)):
+        p, s = c.slots(b, lens[b])
+        assert (w[p, :, s] != c.weights[p, :, s]).float().mean() > 0.9
+    h.close()
+
+
 # ---------------------------------------------------------------- prefill
 
 # segments (rows, cached tokens), chunk, query heads, kv heads, head dim
