@@ -372,6 +372,24 @@ def test_select_long(length):
         run_select(c, length // 3, 100)
 
 
+@pytest.mark.parametrize("kind", ["spread", "few", "zero", "close", "odd", "fourth", "rising", "wide"])
+@pytest.mark.parametrize("length", [8200, 12288, 16384, 20001, 32768])
+def test_select_long_kinds(length, kind):
+    """Weights of which some, by their place, say something else than all do."""
+    c = ec.Cache([length, 9], 1, 64, 126)
+    if kind in ("fourth", "rising", "wide"):
+        j = torch.arange(16 * c.blocks, dtype=torch.float32)
+        gen = torch.Generator().manual_seed(127)
+        w = {"fourth": torch.where(j % 4 == 0, 2.0, 1e-3) * (1 + torch.rand(j.shape, generator=gen)), "rising": j / 1000 - 3,
+             "wide": torch.exp2(200 * torch.rand(j.shape, generator=gen) - 100) * torch.where(torch.rand(j.shape, generator=gen) < 0.3, -1.0, 1.0)}[kind]
+        pages, places = c.slots(0, length)
+        c.weights[pages, 0, places] = w[:length]
+    else:
+        fill_weights(c, kind, 128)
+    for keep, recent in ((1, 0), (101, 3), (length // 8, 256), (length // 4, 0), (length // 2, 0), (length - 1, 7)):
+        run_select(c, keep, recent)
+
+
 def test_select_under_the_largest_bound():
     c = ec.Cache([1000, 70], 1, 64, 124, extra_blocks=(1 << 19) // 16)
     fill_weights(c, "spread", 125)
