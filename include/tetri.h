@@ -501,8 +501,8 @@ TETRI_API tetri_status tetri_decode_attn_weights(tetri_ctx *ctx, const void *q, 
  *     new_lens [num_reqs] int32: n, the ctx_lens after tetri_kv_compact (another array than ctx_lens)
  * So as few tokens move as can, and the last r slots are the newest r tokens, oldest first, again.
  *   kv_weights, block_table [num_reqs][max_blocks_per_seq], ctx_lens: device, in.  slots (16-byte aligned), new_lens: device, out.
- *   max_ctx_len: an upper bound of ctx_lens; of a longer request only the first max_ctx_len slots count.  1 <= keep <=
- *   max_blocks_per_seq * page_size, 0 <= recent <= keep.
+ *   max_ctx_len: an upper bound of ctx_lens; of a longer request only the first max_ctx_len slots count, as if it had no more
+ *   (L = max_ctx_len above).  1 <= keep <= max_blocks_per_seq * page_size, 0 <= recent <= keep.
  * TETRI_ERR_UNSUPPORTED for max_ctx_len above 524288.
  */
 TETRI_API tetri_status tetri_kv_select(tetri_ctx *ctx, const float *kv_weights, const int32_t *block_table, const int32_t *ctx_lens,
@@ -511,7 +511,8 @@ TETRI_API tetri_status tetri_kv_select(tetri_ctx *ctx, const float *kv_weights, 
 
 /*
  * Moves the tokens that stay, in place: afterwards slot i < n of request b and a kv head holds what slot slots[b][head][i] held, K, V
- * and weight; slots at and behind n hold nothing of meaning (those at and behind the old ctx_lens[b] are not touched).
+ * and weight, with n = new_lens[b]; slots at and behind n hold nothing of meaning (those at and behind the old ctx_lens[b] are not
+ * touched).  So a request that was longer than tetri_kv_select's max_ctx_len loses the tokens behind that too.
  *   slots, block_table, ctx_lens (as it was for tetri_kv_select, not new_lens), num_reqs, keep, recent: as for tetri_kv_select, whose
  *   map it has to be (of another one no more is promised than that no slot but the requests' own is read or written).
  *   kv_pages, kv_weights: device, in/out.  fp8: 1 = kv_pages is a pool of E4M3 codes.

@@ -428,9 +428,12 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const int32_t 
     __shared__ int32_t wave_moves[kCompactThreads / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lane_row = tid / LPR, chunk = tid % LPR;
     const int rest = blockIdx.x / Hkv, kh = blockIdx.x - rest * Hkv, b = rest / (tiles + 2), tile = rest - b * (tiles + 2) - 2;
-    const int L = min(max(ctx[b], 0), max_blocks * kPage), n = min(L, keep), r = min(recent, n), heavy = n - r, e = L - n;
-    if (e == 0) return;
     const int32_t *map = slots + ((size_t)b * Hkv + kh) * keep, *row = bt + (size_t)b * max_blocks;
+    // how far the newest tokens come is the map's to say, not the length's: of a request longer than the max_ctx_len it was made under, the
+    // tokens behind that are given up too
+    const int newest = tile < 0 ? map[keep - 1] : 0;
+    const int L = min(max(ctx[b], 0), max_blocks * kPage), n = keep, r = recent, heavy = n - r;
+    if (L <= n) return;
     auto data = [&](int page, int slot, int kv) -> char * {
         return pages + ((((size_t)page * 2 + kv) * Hkv + kh) * kPage + slot) * RB + chunk * 16;
     };
@@ -488,7 +491,8 @@ __global__ __launch_bounds__(kCompactThreads) void compact_kernel(const int32_t 
         }
         return;
     }
-    const int kv = tile + 2;
+    if (newest < n || newest >= L) return;               // (the map moves nothing: no more than `keep` were chosen from)
+    const int kv = tile + 2, e = newest - (n - 1);
     const bool weighs = kv == 0 && chunk == 0;           // these lanes move the weights as well
     for (int base = 0; base < r; base += kBack) {
         const int many = min(r - base, kBack);
