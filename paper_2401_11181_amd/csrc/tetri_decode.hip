@@ -633,6 +633,8 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
         }
     }
     bool finished = whole;
+    [[maybe_unused]] int said = 0;                       // W: the request's length as the caller has it (job.L is what the block table can describe)
+    if constexpr (W) said = ((const const_i32 *)(uintptr_t)ctx_lens)[job.b];
     if (!whole) {
         coherent_stores_done();
         lds_barrier();
@@ -725,7 +727,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
             const float *scores = e->scores + head * stride;
             typedef __attribute__((address_space(1))) f32x4 global_f32x4;
             const int slots = job.L + append;            // (the host sees to it that max_ctx leaves a slot for the new token)
-            if (job.L <= e->max_ctx)                     // (not longer than the caller said)
+            if (said <= e->max_ctx)                      // (not longer than the caller said)
                 for (int j = 4 * te; j < slots; j += 4 * NT) {
                     float *at = e->weights_w + ((size_t)table[j / kPage] * Hkv + kh) * kPage + j % kPage;
                     f32x4 x = *reinterpret_cast<global_f32x4 *>((uintptr_t)at);

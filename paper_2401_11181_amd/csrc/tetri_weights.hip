@@ -26,8 +26,8 @@ __global__ __launch_bounds__(256) void add_weights_kernel(AddWeightsParams p)
 {
     const int kh = blockIdx.y;
     for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
-        const int L = p.ctx[b];
-        if (L < 0 || L > p.max_ctx) continue;            // (longer than the caller said)
+        const int L = max(p.ctx[b], 0);                  // (a length below 0 is 0, as for the attention and the cache)
+        if (L > p.max_ctx) continue;                     // (longer than the caller said)
         const int j = blockIdx.x * kAddKeys + threadIdx.x * 4;
         const size_t head = (size_t)b * p.Hq + (size_t)kh * p.g;
         if (j < L) {
