@@ -459,6 +459,7 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
  *     ctx_lens[s] <= j < ctx_lens[s]+n_s:  kv_weights at slot j  = w_j    (the chunk's own tokens; whether or not tetri_kv_append
  *                                          has run), also where w_j = 0
  * K_s as for tetri_chunk_prefill_attn: kv_pages for j < ctx_lens[s], k_new otherwise.  last_rows >= chunk_size counts every row.
+ * A row whose softmax is NaN (NaN or infinities among its scores) makes NaN of the keys it sees and of no others.
  *   q [chunk_size][num_q_heads][head_dim], k_new [chunk_size][num_kv_heads][head_dim], kv_pages, block_table, cu_chunk_q_lens,
  *   ctx_lens: device, in.  kv_weights: device, in/out.  fp8: 1 = kv_pages is a pool of E4M3 codes under k_scale (otherwise
  *   ignored); k_new is bf16 either way.  num_segs: 1..max_segs_per_chunk.  last_rows >= 1.

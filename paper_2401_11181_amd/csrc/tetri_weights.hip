@@ -483,10 +483,12 @@ __global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const
     constexpr int MY = T::NI / 4;
     __shared__ __attribute__((aligned(1024))) char ring[DEPTH * kStreamBytes];
     __shared__ __attribute__((aligned(16))) float minus_lse[2 * BATCH];   // of this batch of rows and the one before
+    __shared__ int no_sum[2];                            // last row that has no finite sum (-1: none), of this item and the one before
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, l32 = lane & 31;
     const int kh = blockIdx.x % Hkv;
     const uint32_t base = tile_base<D, false>(lane), ring_lds = lds_address(ring);
-    for (int item = blockIdx.x / Hkv;; item += gridDim.x / Hkv) {
+    if (tid < 2) no_sum[tid] = -1;
+    for (int item = blockIdx.x / Hkv, turn = 0;; item += gridDim.x / Hkv, turn ^= 1) {
         Segment x;
         if (!find_segment(Lookup{cu, ctx, S, C, max_tokens, max_ctx, last, g}, item, lane,
                           [&](int n, int L) { return (L + KEYS - 1) / KEYS + (n + KEYS - 1) / KEYS; }, x)) return;
@@ -539,6 +541,7 @@ __global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const
             }
         };
         lds_barrier();                                   // (everybody is done with the item before)
+        if (tid == 0) no_sum[turn ^ 1] = -1;             // (of the item before, for the next one)
 #pragma unroll
         for (int i = 0; i < DEPTH - 1; ++i) issue(i);
         bf16x8 kf[SUB][KSTEPS];
@@ -552,10 +555,17 @@ __global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const
             load_key<D, FP8>(p, x, kh, cached, page, key, half, kf[b]);
             sum_before[b] = cached ? *weight[b] : 0.f;
         }
-        // minus the logarithms of 256 rows' sums, from row r0 on; rows past the end: -infinity, that is weight 0
+        // minus the logarithms of 256 rows' sums, from row r0 on; rows past the end: -infinity, that is weight 0.  So are rows whose sum is NaN or
+        // infinite, for what such a row gives is NaN, also to keys that it does not see; those that see the last of these get NaN at the end.
         auto sums = [&](int r0, float *to_lds) {
             const int r = r0 + tid;
-            to_lds[tid] = r < x.rows ? -p.lse[query_row(p, x, kh, r)] : -INFINITY;
+            float minus = -INFINITY;
+            if (r < x.rows) {
+                const float lse = p.lse[query_row(p, x, kh, r)];
+                if (fabsf(lse) < INFINITY) minus = -lse;
+                else atomicMax(&no_sum[turn], r);
+            }
+            to_lds[tid] = minus;
         };
         if (steps > 0) sums(from * 32, minus_lse);
 #pragma unroll
@@ -617,7 +627,8 @@ __global__ __launch_bounds__(256, SUB == 2 ? 2 : 3) void weigh_keys_kernel(const
         wait_vm<0>();
 #pragma unroll
         for (int b = 0; b < SUB; ++b) {
-            const float total = half_swap_sum(sum[b]);
+            float total = half_swap_sum(sum[b]);
+            if (max(first_row[b], 0) <= no_sum[turn]) total = NAN;
             if (half == 0 && key0 + 32 * b + l32 < keys) *weight[b] = sum_before[b] + total;
         }
     }
