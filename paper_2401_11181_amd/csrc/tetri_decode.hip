@@ -736,6 +736,7 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                         for (int i = 0; i < 4; ++i)
                             if (j + i == job.L) x[i] = 0.f;
                     }
+                    f32x4 given = {0.f, 0.f, 0.f, 0.f};  // (summed by itself: added to x, which may be large, head by head it could vanish)
                     for (int h = 0; h < g; ++h) {
                         const float2 lo = load_coherent2(scores + (size_t)h * stride + j), hi = load_coherent2(scores + (size_t)h * stride + j + 2);
                         const float t[4] = {lo.x, lo.y, hi.x, hi.y};
@@ -745,9 +746,11 @@ __global__ __launch_bounds__(NW * 64, 2) void decode_attn_kernel(const int32_t *
                             if constexpr (FP8) {
                                 if (j + i == job.L) s = load_coherent(e->new_scores + head + h);
                             }
-                            x[i] += __builtin_amdgcn_exp2f(s - log_sum[h]);
+                            given[i] += __builtin_amdgcn_exp2f(s - log_sum[h]);
                         }
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] += given[i];
                     if (j + 4 <= slots) {
                         *reinterpret_cast<global_f32x4 *>((uintptr_t)at) = x;
                     } else {

@@ -34,12 +34,15 @@ __global__ __launch_bounds__(256) void add_weights_kernel(AddWeightsParams p)
             float *w = p.weights + ((size_t)p.bt[(size_t)b * p.max_blocks + j / kPage] * p.Hkv + kh) * kPage + j % kPage;
             f32x4 x = *reinterpret_cast<global_f32x4 *>((uintptr_t)w);
             const float *row = p.scores + head * p.score_stride + j;
+            f32x4 given = {0.f, 0.f, 0.f, 0.f};          // (summed by itself: added to x, which may be large, head by head it could vanish)
             for (int h = 0; h < p.g; ++h, row += p.score_stride) {
                 const f32x4 t = *reinterpret_cast<global_f32x4 *>((uintptr_t)row);
                 const float lse = p.lse[head + h];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] += j + i < L ? __builtin_amdgcn_exp2f(t[i] - lse) : 0.f;
+                for (int i = 0; i < 4; ++i) given[i] += j + i < L ? __builtin_amdgcn_exp2f(t[i] - lse) : 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] += given[i];
             if (j + 4 <= L) {
                 *reinterpret_cast<global_f32x4_w *>((uintptr_t)w) = x;
             } else {
