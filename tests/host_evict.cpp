@@ -299,6 +299,51 @@ void arguments()
     tetri_destroy(h);
 }
 
+// The kernels that shapes of tests/test_gpu_evict_instances.py go to on 256 compute units (those tests are there to run these kernels).
+void instances()
+{
+    struct { int hq, hkv, chunk, segs, max_ctx, last, row_waves, parts, wide; } const weighs[] = {
+        {32, 8, 512, 1, 16384, 32, 2, 64, 1},
+        {32, 8, 512, 7, 3000, 1000, 2, 3, 0},
+        {192, 48, 256, 1, 600, 1000, 4, 2, 0},
+        {48, 48, 1000, 1, 33, 1000, 4, 2, 0},
+        {96, 24, 480, 3, 700, 1000, 4, 2, 0},
+        {192, 48, 480, 3, 1700, 1000, 4, 1, 1},
+        {192, 48, 300, 1, 1500, 130, 4, 3, 0},
+        {96, 24, 203, 3, 1200, 1000, 2, 2, 0},
+        {144, 48, 145, 2, 2600, 1000, 2, 2, 1},
+        {48, 48, 16, 1, 2600, 1000, 1, 10, 1},
+    };
+    for (const auto &x : weighs)
+        for (int d : {64, 128})
+            for (int fp8 : {0, 1}) {
+                tetri_ctx *h = handle(x.hq, x.hkv, d, x.chunk, 2048);
+                Args a;
+                a.n = x.segs; a.max_ctx = x.max_ctx; a.last = x.last; a.fp8 = fp8;
+                CHECK(weigh(h, a) == TETRI_OK);
+                CHECK(g_weigh.row_waves == x.row_waves && g_weigh.parts == x.parts && g_weigh.wide_keys == x.wide);
+                tetri_destroy(h);
+            }
+    // decode: ranges, parts, and by default; the weights by the launch itself and by one behind it
+    struct { int n, max_ctx; const char *option; int value, added; } const decodes[] = {
+        {5, 2100, nullptr, 0, 1}, {5, 2100, "decode_ranges", 7, 1}, {5, 2100, "decode_parts", 3, 1}, {3, 2100, nullptr, 0, 1},
+        {1, 1000, nullptr, 0, 0}, {6, 260, nullptr, 0, 0}, {3, 260, nullptr, 0, 0},
+    };
+    for (const auto &x : decodes)
+        for (int fp8 : {0, 1}) {
+            tetri_ctx *h = handle();
+            if (x.option) CHECK(tetri_set_option(h, x.option, x.value) == TETRI_OK);
+            Args a;
+            a.n = x.n; a.max_ctx = x.max_ctx; a.fp8 = fp8;
+            g_added = false;
+            CHECK(decode(h, a) == TETRI_OK && g_added == (x.added != 0));
+            if (x.option && !std::strcmp(x.option, "decode_ranges")) CHECK(g_decode.parts == 0 && g_decode.ranges == x.value);
+            if (x.option && !std::strcmp(x.option, "decode_parts")) CHECK(g_decode.parts == x.value);
+            if (x.added) CHECK((g_add.new_scores != nullptr) == (fp8 != 0));
+            tetri_destroy(h);
+        }
+}
+
 }  // namespace
 
 int main(int argc, char **argv)
@@ -307,6 +352,7 @@ int main(int argc, char **argv)
     if (name == "refusals") refusals();
     else if (name == "workspaces") workspaces();
     else if (name == "arguments") arguments();
+    else if (name == "instances") instances();
     else return 2;
     std::printf("%s: ok\n", name.c_str());
     return 0;

@@ -28,3 +28,9 @@ def driver(tmp_path_factory):
 def test_host_layer(driver, check):
     res = subprocess.run([driver, check], capture_output=True, text=True, timeout=120)
     assert res.returncode == 0 and check + ": ok" in res.stdout, res.stdout + res.stderr
+
+
+def test_kernels_of_the_gpu_tests(driver):
+    """The shapes of tests/test_gpu_evict_instances.py go to the kernels that they are meant for."""
+    res = subprocess.run([driver, "instances"], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0 and "instances: ok" in res.stdout, res.stdout + res.stderr
