@@ -439,16 +439,28 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
  * The state is one float per slot, for the caller to keep beside kv_pages and to use with the same block tables:
  *     kv_weights [num_pages][num_kv_heads][page_size] float: the softmax weight the token in that slot has received so far, from
  *                all the query heads that share the kv head; 16-byte aligned
- * Slots that hold no token yet need no value.  The calls:
- *   tetri_chunk_prefill_weights  adds what rows of a prefill chunk give          \ either or both, in any order with the calls
- *   tetri_decode_attn_weights    a decode iteration that adds what it gives      / that append
+ * The calls:
+ *   tetri_chunk_prefill_weights  adds what rows of a prefill chunk give; before or after the chunk's attention and append
+ *   tetri_decode_attn_weights    a decode iteration that adds what it gives
  *   tetri_kv_select              which slots of every request and kv head stay
  *   tetri_kv_compact             moves what stays to the front of the cache; ctx_lens shrinks, pages behind it are free again
+ * What a slot has to hold, and who sees to it:
+ *   - The weighing calls write the weight of a token that comes with them (a row of the chunk, the decoded token with append = 1):
+ *     its slot needs no value before.  To those of all cached tokens they add.
+ *   - A token that comes into the cache by another call (tetri_kv_append or a fused append without a weighing call for the same
+ *     rows, tetri_kv_import, tetri_decode_attn_weights with append = 0 and an append) has what its slot happens to hold, such as the
+ *     weight of a token that was given up: the caller writes a weight there, as a rule 0, before the next of these calls.  It is enough
+ *     to write 0 to a request's pages when it gets them, and after tetri_kv_compact to its slots [new_lens, ctx_lens).
+ *   - In one weighing call no two requests (segments) may have a page in common: each adds to what it has read, and one's additions
+ *     would be lost (`out` and the pool are right all the same).  Requests that share the pages of a prefix are weighed by calls one
+ *     after the other, which add up; they cannot be compacted.
+ *   - tetri_kv_export and tetri_kv_import carry K and V.  Weights follow a request to another pool by a copy of its pages of
+ *     kv_weights, page block_table[b][i] of one pool to page block_table[b][i] of the other.
  * The kv heads of a request keep the same number of tokens, not the same tokens.  Attention does not depend on the order of the
  * cache, so afterwards every call works as before on the shorter cache; position information is in K itself and stays.
- * Scores, exponentials, sums and weights are fp32.  Results are deterministic run to run.  The calls use the caller's workspace
- * where they need any (16-byte aligned device memory, contents of no meaning before and after): calls that may overlap in time,
- * and graphs whose replays may, need one each.
+ * Scores, exponentials, sums and weights are fp32.  Results are deterministic run to run.  The weighing calls use the caller's workspace
+ * (16-byte aligned device memory, contents of no meaning before and after): calls that may overlap in time, and graphs whose replays
+ * may, need one each.
  */
 
 /*
@@ -463,7 +475,8 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
  *   q [chunk_size][num_q_heads][head_dim], k_new [chunk_size][num_kv_heads][head_dim], kv_pages, block_table, cu_chunk_q_lens,
  *   ctx_lens: device, in.  kv_weights: device, in/out.  fp8: 1 = kv_pages is a pool of E4M3 codes under k_scale (otherwise
  *   ignored); k_new is bf16 either way.  num_segs: 1..max_segs_per_chunk.  last_rows >= 1.
- *   max_ctx_len: host scalar, an upper bound of ctx_lens; a segment whose context is longer is left out.
+ *   max_ctx_len: host scalar, an upper bound of ctx_lens; a segment whose context is longer is left out (no weight is written for its
+ *   own tokens either).
  *   workspace: at least tetri_chunk_prefill_weights_workspace(num_segs, max_ctx_len, last_rows) bytes (a negative tetri_status for
  *   arguments that the call would refuse).
  * Errors as for tetri_chunk_prefill_attn; TETRI_ERR_INVALID_ARG also for a workspace that is too small.
@@ -479,7 +492,8 @@ TETRI_API tetri_status tetri_chunk_prefill_weights(tetri_ctx *ctx, const void *q
  * tetri_decode_attn_append (fp8 = 1: tetri_decode_attn_fp8 under k_scale and v_scale), and for every request b, kv head and slot
  * j < ctx_lens[b] the weight that the new token's query heads give to K_b[j] is added to kv_weights; with append = 1 what they give to
  * the new token itself becomes the weight of its slot, ctx_lens[b].
- *   max_ctx_len is an upper bound of ctx_lens here in earnest: of a request that is longer no weight is added.
+ *   max_ctx_len is an upper bound of ctx_lens here in earnest: of a request that is longer no weight is added or,
+ *   for its new token, written.
  *   workspace: at least tetri_decode_attn_weights_workspace(num_reqs, max_ctx_len) bytes (a negative tetri_status for arguments that
  *   the call would refuse).
  * Other arguments, errors and the scratch-memory rule as for those calls.

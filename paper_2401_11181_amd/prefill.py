@@ -112,7 +112,8 @@ class ChunkedPrefill:
 
     def weights(self, c, q, k_new, kv_pages, kv_weights, scale, last_rows, workspace, k_scale=None, stream=None):
         """Adds to kv_weights what the last rows of chunk c's segments give to the keys.  k_scale: that of a pool of FP8 codes
-        (None: a 16-bit pool)."""
+        (None: a 16-bit pool).  The chunk's own tokens get their weight by this; those of chunks that are not weighed need one,
+        as a rule 0, from the caller."""
         cu, ctx, bt, S = self.meta[c]
         self.handle.tetri_chunk_prefill_weights(q, k_new, kv_pages, kv_weights, bt, cu, ctx, S, self._longest_ctx(c), last_rows, scale,
                                                 int(k_scale is not None), 1.0 if k_scale is None else k_scale, workspace,
