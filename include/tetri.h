@@ -514,7 +514,7 @@ TETRI_API tetri_status tetri_decode_attn_weights(tetri_ctx *ctx, const void *q, 
  *                  i >= n - r:  i + L - n
  *       i >= n:                 -1
  *     new_lens [num_reqs] int32: n, the ctx_lens after tetri_kv_compact (another array than ctx_lens)
- * So as few tokens move as can, and the last r slots are the newest r tokens, oldest first, again.
+ * So the last r slots are the newest r tokens, oldest first, again, and of the others as few move as can.
  *   kv_weights, block_table [num_reqs][max_blocks_per_seq], ctx_lens: device, in.  slots (16-byte aligned), new_lens: device, out.
  *   max_ctx_len: an upper bound of ctx_lens; of a longer request only the first max_ctx_len slots count, as if it had no more
  *   (L = max_ctx_len above).  1 <= keep <= max_blocks_per_seq * page_size, 0 <= recent <= keep.

@@ -5,8 +5,8 @@
 //   * a kept slot below n - r stays where it is;
 //   * the k-th slot below n - r that is not kept (a hole) takes the k-th kept slot of [n - r, L - r): there are as many of each;
 //   * slot n - r + i takes slot L - r + i: the newest tokens close up, in their order.
-// So as few tokens move as can (attention does not care for the order of the others), and the last slots are the newest tokens again,
-// which is all that the next eviction needs to know.
+// So the last slots are the newest tokens again, which is all that the next eviction needs to know, and of the others, for whose order attention
+// does not care, as few move as can.  (The newest all do, by e slots, however few are given up.)
 #include "attn_common.h"
 
 namespace {
