@@ -123,7 +123,8 @@ __device__ __forceinline__ bool find_segment(const Lookup &p, int tile, int lane
 // products, the vector pipe as many for its 2048 exponentials (8 cycles per 64 of them) with an addition and a multiplication-addition
 // each.  So that both are at work, the products of one block of 32 x 32 scores stand between the exponentials of the block before, a matrix
 // instruction to two elements.  (2048 rows behind 14336 tokens, 32/8 heads, where the card's power is what bounds it: 535 us, 470 if all
-// values are the same; one after the other 579.  Two products of that size by the library's rate for large matrices: 432.)
+// values are the same; one after the other 579; 528 to 606 on different cards.  Two products of that size by the library's rate for large
+// matrices: 432.)
 constexpr int kSub = 2;                  // blocks of 32 rows that a wavefront keeps
 constexpr int kStreamBytes = 8192;       // a tile of 32 rows of 128 16-bit values
 
