@@ -105,3 +105,13 @@ def test_new_key():
     def spoil(q, k, c, cu):
         k[17, 0, 5] = float("nan")
     run([(60, 90), (30, 70)], 4, 2, 128, 1000, 205, False, spoil)
+
+
+def test_workgroups_that_go_over_many_segments():
+    """More tiles of keys than workgroups abreast: what one segment's rows leave behind is none of the next one's."""
+    segs = [(20 + i % 5, 3 * i) for i in range(30)]
+
+    def spoil(q, k, c, cu):
+        for s in range(0, 30, 3):
+            q[cu[s] + s % 20, s::7, 1] = float("nan")
+    run(segs, 64, 64, 64, 1000, 206, False, spoil)
