@@ -16,7 +16,7 @@ HQ, HKV, D, SCALE = 4, 2, 64, 0.125
 class Run:
     """Requests of which nothing is cached yet, in a pool and weights of garbage; calls of the library beside the oracle's."""
 
-    def __init__(self, tokens, seed, fp8, max_blocks=None):
+    def __init__(self, tokens, seed, fp8):
         self.c = c = ec.Cache([0] * len(tokens), HKV, D, seed, fp8, room=tokens, extra_blocks=0)
         self.gen, self.fp8, self.B = torch.Generator().manual_seed(seed + 1), int(fp8), len(tokens)
         self.pool, self.w, self.bt = dev(c.pool.clone()), dev(c.weights.clone()), dev(c.bt)
