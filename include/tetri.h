@@ -434,6 +434,74 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
                                                     int32_t append, void *out, void *stream);
 
 /*
+ * Cache held in 4 bits (the same kind of extension: a little over a quarter of the bytes of the 16-bit cache, on the link and in memory).
+ * Format: OCP microscaling MXFP4.  32 neighbouring elements of a row of K or V, a group, share a power of two 2^(e - 127), e a byte; each element is an
+ * E2M1 code: bits 0..2 stand for 0, 0.5, 1, 1.5, 2, 3, 4, 6, bit 3 is the sign.  A value x of a group is stored as follows: e - 127 =
+ * max(floor(log2 of the group's largest magnitude) - 2, -127), the code is that of x / 2^(e - 127) rounded to nearest, of two equally near ones the
+ * even code, magnitudes above 6 to 6 (a group of zeros: e = 0).  In a group with an infinity or a NaN e is 255 and all codes are 0; e = 255
+ * makes NaN of every element.  No scale is a caller's argument.
+ *   pool kv_pages_fp4 [num_pages][2][num_kv_heads] blocks of 16 * head_dim * 17 / 32 bytes, 16-byte aligned: 16 rows of head_dim / 2 bytes of codes, the even
+ *   element in bits 0..3 of a byte, then 16 rows of head_dim / 32 bytes, the e of the row's groups.
+ *   buffer of export and import: request r's block begins at byte 2 * num_kv_heads * (head_dim * 17 / 32) * cu_tokens[r] and holds the codes
+ *   [2][num_kv_heads][n_r][head_dim / 2] and then the e [2][num_kv_heads][n_r][head_dim / 32].
+ *
+ * tetri_kv_export_fp4: as tetri_kv_export from the 16-bit pool, quantising.  tetri_kv_import_fp4: scatters such a buffer into a pool of codes, bit
+ *   for bit.
+ * tetri_decode_attn_fp4, tetri_chunk_prefill_attn_fp4: tetri_decode_attn and tetri_chunk_prefill_attn over such a pool.  The new token's or the chunk's
+ *   own k_new / v_new (bf16) enter unquantised; with append = 1 their codes are also written to their slots of the pool (then kv_pages_fp4 is
+ *   in/out and block_table must cover them), with append = 0 the pool is only read.  Cached values become bf16 exactly (below 2^-133: 0).
+ * Other arguments, errors, the limits and the scratch-memory rule as for the 16-bit calls.  tetri_kv_select and what belongs to it have no form for
+ * such a pool, nor have the calls with host metadata.
+ */
+TETRI_API tetri_status tetri_kv_export_fp4(tetri_ctx *ctx, const void *kv_pages, const int32_t *block_table,
+                                           const int32_t *cu_tokens, const int32_t *first_tokens, int32_t num_reqs,
+                                           int64_t total_tokens, void *buf, void *stream);
+TETRI_API tetri_status tetri_kv_import_fp4(tetri_ctx *ctx, const void *buf, const int32_t *block_table,
+                                           const int32_t *cu_tokens, const int32_t *first_tokens, int32_t num_reqs,
+                                           int64_t total_tokens, void *kv_pages_fp4, void *stream);
+TETRI_API tetri_status tetri_decode_attn_fp4(tetri_ctx *ctx, const void *q, const void *k_new, const void *v_new,
+                                             void *kv_pages_fp4, const int32_t *block_table, const int32_t *ctx_lens,
+                                             int32_t num_reqs, int32_t max_ctx_len, float scale, int32_t append, void *out,
+                                             void *stream);
+TETRI_API tetri_status tetri_chunk_prefill_attn_fp4(tetri_ctx *ctx, const void *q, const void *k_new, const void *v_new,
+                                                    void *kv_pages_fp4, const int32_t *block_table,
+                                                    const int32_t *cu_chunk_q_lens, const int32_t *ctx_lens,
+                                                    int32_t num_segs, float scale, int32_t append, void *out, void *stream);
+
+/*
+ * Queries and keys made ready for the attention calls (an extension of this build: the paper's path begins behind it): RMS norm of every head
+ * and rotation by position, out of the rows of a projection into the contiguous rows that those calls take.
+ * For every row and head of q (k alike, with k_weight)
+ *     y_i = x_i * q_weight[i] / sqrt(mean of x_j^2 over the head + eps)            (y = x where q_weight is NULL)
+ *     pair i < num_pairs is (y_i, y_{i + num_pairs}), or (y_2i, y_{2i+1}) with adjacent = 1; it is turned by the angle
+ *     t_i = freq[i] * (the row's position on axis[i]):   (a cos t - b sin t, b cos t + a sin t)
+ * and elements that belong to no pair stay y.  The angle is taken in 64 bits; the rest is fp32, rounded once to bf16 (nearest even).
+ * The row's position: with `positions` positions[axis][row] (any int32), for images and video three axes for instance; otherwise row t of segment s of a
+ * chunk has position ctx_lens[s] + t on all axes, and rows at and behind cu_chunk_q_lens[num_segs] are neither read nor written.
+ *   q, k: device, in: rows of q_stride and k_stride elements (multiples of 8), of which the first num_q_heads * head_dim and
+ *   num_kv_heads * head_dim are taken: parts of a fused projection, for instance.  q_weight, k_weight [head_dim] bf16: device, or NULL.
+ *   rope: host, read before the call returns.  Exactly one of positions [num_axes][num_rows] and (cu_chunk_q_lens, ctx_lens) is given, device;
+ *   num_segs: 1..max_segs_per_chunk with the latter.  num_rows >= 1 (not bound by chunk_size).
+ *   q_out [num_rows][num_q_heads][head_dim], k_out [num_rows][num_kv_heads][head_dim]: device, out.  Each may be its input where that has no gaps
+ *   between its rows; otherwise outputs and inputs must not overlap.
+ * Uses none of the handle's scratch memory.  TETRI_ERR_INVALID_ARG for null or misaligned pointers, strides and counts out of range, num_pairs that is no
+ * multiple of 8 of at most head_dim / 2, an axis that is not below num_axes, a frequency or eps that is not finite.
+ */
+enum { TETRI_ROPE_PAIRS = 64 };
+typedef struct {
+    int32_t num_pairs;            /* pairs of a head that turn: a multiple of 8, at most head_dim / 2 */
+    int32_t num_axes;             /* 1..8                                                             */
+    int32_t adjacent;             /* 1: pairs are neighbours; 0: num_pairs elements apart             */
+    float freq[TETRI_ROPE_PAIRS]; /* radians per position, of every pair                              */
+    uint8_t axis[TETRI_ROPE_PAIRS];  /* the axis whose position turns it                              */
+} tetri_rope;
+TETRI_API tetri_status tetri_qk_norm_rope(tetri_ctx *ctx, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                          const void *q_weight, const void *k_weight, float eps, const tetri_rope *rope,
+                                          const int32_t *positions, const int32_t *cu_chunk_q_lens,
+                                          const int32_t *ctx_lens, int32_t num_segs, int32_t num_rows, void *q_out,
+                                          void *k_out, void *stream);
+
+/*
  * Eviction from the paged cache by accumulated attention weight (an extension of this build, not of the paper: Sec. 3.4 names the
  * decode instance's memory as what limits its batch; here a request gives back the slots of tokens that nobody looks at).
  * The state is one float per slot, for the caller to keep beside kv_pages and to use with the same block tables:

@@ -1,8 +1,9 @@
-// Row tiles of the shared-tile attention kernels (tetri_attn.hip, tetri_planned.hip): one job of a workgroup.
+// Row tiles of the shared-tile attention kernels (tetri_attn.hip, tetri_planned.hip): one job of a workgroup.  BITS: of an element of the pool,
+// 16 (bf16), 8 (E4M3 codes) or 4 (microscaled E2M1 codes).
 #pragma once
 #include <type_traits>
 
-#include "attn_common.h"
+#include "cache_fp4.h"
 
 namespace tetri_dev {
 
@@ -104,17 +105,17 @@ struct WaveSrc {
     int max_blocks;
 };
 
-template <int D, int KS, bool F8>
+template <int D, int KS, int BITS>
 __device__ __forceinline__ WaveSrc make_wave_src(const AttnParams &p, int kh)
 {
-    constexpr int ESZ = F8 ? 1 : 2;                    // bytes of a pool element
+    constexpr uint32_t SLAB = slab_bytes<D, BITS>();
     WaveSrc ws;
     ws.bt = p.bt;
     ws.new_k = reinterpret_cast<const char *>(p.k_new);
     ws.new_v = reinterpret_cast<const char *>(p.v_new);
-    ws.pool_k = reinterpret_cast<const char *>(p.pages) + (size_t)kh * (kPage * D * ESZ);
-    ws.page_bytes = 2 * p.Hkv * (kPage * D * ESZ);
-    ws.v_delta = p.Hkv * (kPage * D * ESZ);
+    ws.pool_k = reinterpret_cast<const char *>(p.pages) + (size_t)kh * SLAB;
+    ws.page_bytes = 2 * p.Hkv * SLAB;
+    ws.v_delta = p.Hkv * SLAB;
     ws.stage_new_bytes = Shape<KS>::STAGE * (p.Hkv * D * 2);
     ws.wave_new_bytes = 16 * (p.Hkv * D * 2);
     ws.max_blocks = p.max_blocks;
@@ -129,11 +130,11 @@ struct StageLoads {
     uint32_t kdst;              // LDS byte address of the K rows; the V rows are 2 * STAGE_BYTES further
     int j0, limit;              // first key row, and the end of the key range it belongs to
     uint32_t ko, vo;            // per-lane byte offsets of the first instruction's rows, K and V
-    bool codes;                 // the rows are FP8 codes of a pool of codes: they travel through registers (fetch_stage_codes)
+    bool codes;                 // the rows are codes of a pool of codes: they travel through registers (fetch_stage_codes)
 };
 
 // Where stage `it` of a job comes from.  Returns whether all 16 rows exist.
-template <int D, int KS, bool F8 = false>
+template <int D, int KS, int BITS = 16>
 __device__ __forceinline__ bool describe_stage_loads(const JobSrc &src, const WaveSrc &ws, const LaneOffsets<D> &lo, int page, int it,
                                                      int wave, int new_row_bytes, uint32_t k_lds, StageLoads &sl)
 {
@@ -144,7 +145,7 @@ __device__ __forceinline__ bool describe_stage_loads(const JobSrc &src, const Wa
     sl.j0 = (ctx ? it : jn) * STAGE + 16 * wave;
     sl.limit = ctx ? src.L : src.n_new;
     sl.kdst = k_lds + wave * (16 * D * 2);
-    sl.codes = F8 && ctx;
+    sl.codes = BITS < 16 && ctx;
     // (a lane's row is further away in k_new / v_new, whose rows are Hkv*D*2 bytes apart, than in a page)
     const uint32_t new_extra = ctx ? 0u : (uint32_t)(fresh_lane() / (D / 8)) * (uint32_t)(new_row_bytes - D * 2);
     sl.ko = lo.k_ctx + new_extra;
@@ -195,18 +196,57 @@ __device__ __forceinline__ void issue_stage_loads(const StageLoads &sl, bool ful
     }
 }
 
-// A pool of FP8 codes: the 16 cached key rows a wavefront loads per stage are 16 * D bytes of K and as many of V,
+// A pool of FP8 codes (BITS = 8): the 16 cached key rows a wavefront loads per stage are 16 * D bytes of K and as many of V,
 // each one contiguous (page, kv head) block.  They travel through registers: 16 codes per lane and load (D / 16
 // lanes cover a row), requested where the 16-bit path issues its direct loads and, once arrived, converted to bf16
 // (exactly) and written to the stage buffer in the layout the direct loads produce (write_stage_codes), before
 // the barrier that opens the stage.  The scales are not applied per element (see tile_job).
-template <int D>
+template <int D, int BITS>
 struct StageCodes {
     u32x4 k[D / 64], v[D / 64];
 };
+// A pool of 4-bit codes (cache_fp4.h): the block is 16 * D / 2 bytes of codes and 16 * D / 32 of exponents.  Four lanes cover a row, a lane has D / 4
+// neighbouring values of one scale: one load of codes and one byte of scales each for K and V.  The scale is applied where the codes
+// become bf16, which is exact: such a value is +-{0 .. 6} times a power of two.
+template <int D>
+struct StageCodes<D, 4> {
+    uint32_t k[D / 32], v[D / 32], ks, vs;
+};
 
 template <int D>
-__device__ __forceinline__ void fetch_stage_codes(const StageLoads &sl, bool full, StageCodes<D> &sc)
+__device__ __forceinline__ void fetch_stage_codes(const StageLoads &sl, bool full, StageCodes<D, 4> &sc)
+{
+    const int lane = fresh_lane();
+    // (rows past the end of the cached context hold whatever the pool holds: they read as zeros)
+    const bool ok = full || sl.j0 + lane / 4 < sl.limit;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) sc.k[i] = sc.v[i] = 0u;
+    sc.ks = sc.vs = 0u;
+    if (ok) {
+        load_fp4_codes(sl.kb + lane * (D / 8), sc.k);
+        load_fp4_codes(sl.vb + lane * (D / 8), sc.v);
+        const uint32_t at = kPage * D / 2 + (D == 128 ? lane : lane / 2);
+        sc.ks = load_global_byte(sl.kb + at);
+        sc.vs = load_global_byte(sl.vb + at);
+    }
+}
+
+// kdst: the wavefront's 16 K rows in the stage buffer; its V rows are v_lds bytes further.
+template <int D>
+__device__ __forceinline__ void write_stage_codes(const StageCodes<D, 4> &sc, char *kdst, uint32_t v_lds)
+{
+    constexpr int N = D / 32;                            // 16-byte chunks of a lane's values
+    const int lane = fresh_lane(), r = lane / 4, c0 = N * (lane % 4);
+    char *row = kdst + r * (D * 2);
+    const float ks = fp4_scale(sc.ks), vs = fp4_scale(sc.vs);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(row + (((c0 + i) ^ k_swizzle<D>(r)) << 4)) = fp4_to_bf16(sc.k[i], ks);
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4 *>(row + v_lds + (((c0 + i) ^ v_swizzle<D>(r)) << 4)) = fp4_to_bf16(sc.v[i], vs);
+}
+
+template <int D>
+__device__ __forceinline__ void fetch_stage_codes(const StageLoads &sl, bool full, StageCodes<D, 8> &sc)
 {
     constexpr int NL = D / 64, LPR = D / 16, RPL = 64 / LPR;     // loads per matrix, lanes per row, rows per load
     const int lane = fresh_lane();
@@ -229,7 +269,7 @@ __device__ __forceinline__ void fetch_stage_codes(const StageLoads &sl, bool ful
 
 // kdst: the wavefront's 16 K rows in the stage buffer; its V rows are v_lds bytes further.
 template <int D>
-__device__ __forceinline__ void write_stage_codes(const StageCodes<D> &sc, char *kdst, uint32_t v_lds)
+__device__ __forceinline__ void write_stage_codes(const StageCodes<D, 8> &sc, char *kdst, uint32_t v_lds)
 {
     constexpr int NL = D / 64, LPR = D / 16, RPL = 64 / LPR;
     const int lane = fresh_lane();
@@ -431,12 +471,12 @@ __device__ __forceinline__ void finish_pair(const AttnParams &p, int grp, int wf
 }
 
 // What carries over from one job of a workgroup to the next.
-template <int D>
+template <int D, int BITS>
 struct Carry {
     bf16x8 qf[D / 16];      // Q fragments of the job about to run (requested before the previous job's epilogue)
     int par;                // stage `it` of the job about to run uses stage buffer (it & 1) ^ par
     int page;               // page of this wavefront's rows of the stage after the job's first one
-    StageCodes<D> codes;    // pool of FP8 codes: this wavefront's rows of the job's first stage, if those are cached keys ...
+    StageCodes<D, BITS> codes;    // pool of codes: this wavefront's rows of the job's first stage, if those are cached keys ...
     bool have_codes;        // ... and requested, not yet in the stage buffer
 };
 
@@ -489,10 +529,11 @@ __device__ __forceinline__ void read_q_rows(const char *q_tile, int lane, bf16x8
 
 // The tile's own rows (new keys t0 .. t0 + rows of a tile - 1 of the segment) in the stage buffers go to their page slots:
 // wavefront `wave` takes the 16 rows of each stage it has loaded.  Same result as the stand-alone append kernel, bit for bit.
-template <int D, int KS, bool F8>
+template <int D, int KS, int BITS>
 __device__ __forceinline__ void append_own_rows(const AttnParams &p, const Job &J, const char *smem, int par, int wave)
 {
-    constexpr int CH = D / 8, RPI = 64 / CH, NI = 16 / RPI, ESZ = F8 ? 1 : 2;
+    constexpr int CH = D / 8, RPI = 64 / CH, NI = 16 / RPI, ESZ = BITS / 8;
+    static_assert(BITS >= 8, "no launch on the host's division over 4-bit codes");
     constexpr int STAGE = Shape<KS>::STAGE;
     constexpr uint32_t STAGE_BYTES = STAGE * D * 2;
     const int lane = fresh_lane();
@@ -518,7 +559,7 @@ __device__ __forceinline__ void append_own_rows(const AttnParams &p, const Job &
                     const int slot = off + r;
                     char *dst = pool + (size_t)(slot < kPage ? page0 : page1) * page_bytes + (size_t)mat * p.Hkv * head_bytes
                                 + (size_t)((slot & (kPage - 1)) * CH + c) * (8 * ESZ);
-                    if constexpr (F8) {
+                    if constexpr (BITS == 8) {
                         const uint2 x = bf16_to_codes(v, mat ? p.v_inv : p.k_inv);
                         *reinterpret_cast<global_u32x2_w *>((uintptr_t)dst) = u32x2{x.x, x.y};
                     } else {
@@ -536,9 +577,9 @@ __device__ __forceinline__ void append_own_rows(const AttnParams &p, const Job &
 // all other pieces there merges them and writes the output rows.  Nobody waits for anybody.
 // `next`: the workgroup has a job after this one, N.  On entry the loads of the job's first
 // stage are in flight and cy holds its Q fragments; on exit the same holds for `next`.
-template <int D, int KS, bool F8, bool PLAN>
+template <int D, int KS, int BITS, bool PLAN>
 __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_job, const AttnParams *params, uint4 *smem, float (*Mstat)[2][32],
-                                         uint32_t (*peek)[64], int *old_stash, const Job &J, bool next, const Job &N, Carry<D> &cy,
+                                         uint32_t (*peek)[64], int *old_stash, const Job &J, bool next, const Job &N, Carry<D, BITS> &cy,
                                          Handover &ho)
 {
     constexpr int CH = D / 8;        // 16-byte chunks per K/V row
@@ -556,7 +597,7 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
         p = read_params(params);
     }
     const int grp = J.grp;
-    const WaveSrc ws = make_wave_src<D, KS, F8>(p, J.kh);
+    const WaveSrc ws = make_wave_src<D, KS, BITS>(p, J.kh);
     // The thread id is made opaque per job: values derived from it are then computed where a job
     // needs them instead of being kept in registers across the whole job loop.
     int tid = threadIdx.x;
@@ -620,12 +661,12 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
     // (c: the factor of the block whose weights are being computed; what the change to new keys needs is read from the
     // launch parameters when it happens, once per job, not kept in registers across the stages of cached keys)
     float c = c_new;
-    if constexpr (F8) {
+    if constexpr (BITS == 8) {
         if (J.it_begin < src.n_ctx_tiles) c = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, c_new * p.k_scale)));
     }
     [[maybe_unused]] bool o_scaled = src.n_ctx_tiles == 0;
-    [[maybe_unused]] StageCodes<D> cr = cy.codes;
-    [[maybe_unused]] bool have_codes = F8 && cy.have_codes;
+    [[maybe_unused]] StageCodes<D, BITS> cr = cy.codes;
+    [[maybe_unused]] bool have_codes = BITS < 16 && cy.have_codes;
     const int blk = lane >> 4, i16 = lane & 15;
 
     // Fragment loads from LDS.  K: lane holds key (row) l32 of a 32-key block, d = 16*st + 8*half .. +7
@@ -693,17 +734,19 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
     // the next stage is entered.
     // the loads a StageLoads describes: direct loads into the stage buffer, or codes into registers
     auto issue = [&](const StageLoads &x, bool full) {
-        if (F8 && x.codes) {
-            fetch_stage_codes<D>(x, full, cr);
-            have_codes = true;
-        } else {
-            issue_stage_loads<D, KS>(x, full);
+        if constexpr (BITS < 16) {
+            if (x.codes) {
+                fetch_stage_codes<D>(x, full, cr);
+                have_codes = true;
+                return;
+            }
         }
+        issue_stage_loads<D, KS>(x, full);
     };
     // codes that have arrived go to this wavefront's rows of the buffer of stage `it`, which nobody reads before the
     // barrier that follows
     auto place_codes = [&](int it) {
-        if constexpr (F8) {
+        if constexpr (BITS < 16) {
             if (have_codes) {
                 write_stage_codes<D>(cr, reinterpret_cast<char *>(smem) + buf_of(it) + wave * (16 * D * 2), 2 * STAGE_BYTES);
                 have_codes = false;
@@ -729,7 +772,7 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
     const int32_t *bt_row = ws.bt + src.bt_off;      // the job's block-table row
     auto next_stage_loads = [&](int it, int nb, bool pv_before) {
         if (it + 1 < n_stages) {
-            const bool full = describe_stage_loads<D, KS, F8>(src, ws, lo, page, it + 1, wave, new_row_bytes, smem_lds + (buf_of(it) ^ STAGE_BYTES), sl);
+            const bool full = describe_stage_loads<D, KS, BITS>(src, ws, lo, page, it + 1, wave, new_row_bytes, smem_lds + (buf_of(it) ^ STAGE_BYTES), sl);
             if (full && pv_before && nb != 0 && load_point != 0) pend = true;
             else issue(sl, full);
         }
@@ -776,7 +819,7 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
         // those stores; the announcement follows at the job's second stage (a job of one stage: when its loop is done).
         wait_vm<kPartialStores<D>>();
         place_codes(it);
-        if constexpr (F8) lds_barrier();
+        if constexpr (BITS < 16) lds_barrier();
         else __builtin_amdgcn_s_barrier();
         nblk = stage_blocks(it);
         ho.fresh = false;
@@ -800,7 +843,7 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
     };
     // ... before the first block of new keys
     [[maybe_unused]] auto stage_kind = [&](bool is_ctx) {
-        if constexpr (F8) {
+        if constexpr (BITS == 8) {
             if (!is_ctx && !o_scaled) scale_o();
         }
     };
@@ -1041,10 +1084,10 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
                         st.kdst = smem_lds + cur + wave * (16 * D * 2);
                         st.ko = lo.k_ctx;
                         st.vo = lo.v_ctx;
-                        st.codes = F8;
+                        st.codes = BITS < 16;
                         issue(st, true);
                     } else {
-                        const bool full = describe_stage_loads<D, KS, F8>(src, ws, lo, pg, it + 1, wave, new_row_bytes, smem_lds + cur, st);
+                        const bool full = describe_stage_loads<D, KS, BITS>(src, ws, lo, pg, it + 1, wave, new_row_bytes, smem_lds + cur, st);
                         issue(st, full);
                     }
                 }
@@ -1073,7 +1116,7 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
             if (!block(s_b, s_a)) break;
         }
     }
-    if constexpr (F8) {
+    if constexpr (BITS == 8) {
         if (!o_scaled) scale_o();                      // a stage range of cached keys only: the piece leaves in true units
     }
     // ---- fused append on the host's division: a job whose stages hold the tile's own rows (the last one or two stages of the
@@ -1081,18 +1124,21 @@ __device__ __forceinline__ void tile_job(const AttnParams &kernarg, bool first_j
     if constexpr (PLAN) {
         asm volatile("" ::: "memory");
         const AttnParams pa = read_params(params);
-        if (pa.pages_w != nullptr && J.appends) append_own_rows<D, KS, F8>(pa, J, reinterpret_cast<const char *>(smem), par, wave);
+        if (pa.pages_w != nullptr && J.appends) append_own_rows<D, KS, BITS>(pa, J, reinterpret_cast<const char *>(smem), par, wave);
     }
     // ---- the next job's first stage, into the buffer the job's last stage does not use: every wavefront has left it.
     // The loads travel during this job's epilogue.
     if (next) {
         WaveSrc wsn = ws;                          // (on the host's division the next job may be another head's)
-        if constexpr (PLAN) wsn.pool_k += (ptrdiff_t)(N.kh - J.kh) * (kPage * D * (F8 ? 1 : 2));
-        const bool full = describe_stage_loads<D, KS, F8>(nsrc, wsn, lo, page_n0, n_it_begin, wave, new_row_bytes,
+        if constexpr (PLAN) wsn.pool_k += (ptrdiff_t)(N.kh - J.kh) * slab_bytes<D, BITS>();
+        const bool full = describe_stage_loads<D, KS, BITS>(nsrc, wsn, lo, page_n0, n_it_begin, wave, new_row_bytes,
                                                           smem_lds + (buf_of(n_stages - 1) ^ STAGE_BYTES), sl);
-        cy.have_codes = F8 && sl.codes;
-        if (F8 && sl.codes) fetch_stage_codes<D>(sl, full, cy.codes);     // placed by the next job, before its first barrier
-        else issue_stage_loads<D, KS>(sl, full);
+        cy.have_codes = false;
+        if constexpr (BITS < 16) {
+            cy.have_codes = sl.codes;
+            if (sl.codes) fetch_stage_codes<D>(sl, full, cy.codes);       // placed by the next job, before its first barrier
+        }
+        if (!cy.have_codes) issue_stage_loads<D, KS>(sl, full);
     }
     if (ho.unit >= 0 && (!ho.announced || !stashed)) {        // a partial result not announced, or announced at the job's last stage
         wait_vm<0>();

@@ -57,9 +57,10 @@ using namespace tetri_dev;
 // First every thread looks up where one of the workgroup's rows goes (table in LDS); then rows
 // are copied 8 at a time with all their loads issued before the first store, so that a
 // workgroup has tens of KB in flight.
-// F8: the pool holds FP8 codes; a row's 16-byte vectors (8 values) are quantised on the way (8 codes, 8 bytes) under
-// the tensor's scale; the pool's layout is the same with half the element size.
-template <int D, bool F8>
+// BITS = 8: the pool holds FP8 codes; a row's 16-byte vectors (8 values) are quantised on the way (8 codes, 8 bytes) under
+// the tensor's scale; the pool's layout is the same with half the element size.  BITS = 4: four lanes that have a group of 32 values settle its
+// exponent between them (cache_fp4.h).
+template <int D, int BITS>
 __device__ __forceinline__ void append_rows(const AttnParams &p, unsigned long long *row_dst, int blk, int nblk, int tid, int nthreads)
 {
     constexpr int CH = D / 8, R = 8;
@@ -76,7 +77,9 @@ __device__ __forceinline__ void append_rows(const AttnParams &p, unsigned long l
             const int pos = p.ctx[lo] + (mine - p.cu[lo]);
             const int page = p.bt[(size_t)lo * p.max_blocks + pos / kPage];
             // of the row's K vector 0 of head 0, in units of a vector (16 bytes; 8 bytes of codes)
-            row_dst[tid] = (unsigned long long)page * 2 * p.Hkv * (kPage * CH) + (unsigned long long)(pos % kPage) * CH;
+            // (4-bit codes: page and slot)
+            if constexpr (BITS == 4) row_dst[tid] = (unsigned long long)page * kPage + pos % kPage;
+            else row_dst[tid] = (unsigned long long)page * 2 * p.Hkv * (kPage * CH) + (unsigned long long)(pos % kPage) * CH;
         }
         __syncthreads();
         const int rows_here = min(nthreads, (n_real - base + nblk - 1) / nblk);
@@ -91,8 +94,17 @@ __device__ __forceinline__ void append_rows(const AttnParams &p, unsigned long l
                 for (int r = 0; r < R; ++r) v[r] = src[(size_t)(base + min(r0 + r, rows_here - 1) * nblk) * per_row];
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
+                    if constexpr (BITS == 4) {
+                        static_assert(CH % 4 == 0, "the lanes of a group of 32 values have the same row, and all of them have one");
+                        const unsigned long long place = row_dst[min(r0 + r, rows_here - 1)];
+                        uint32_t exponent;
+                        const uint32_t codes = bf16_to_fp4(v[r], exponent);
+                        char *slab = reinterpret_cast<char *>(p.pages_w) + ((place / kPage * 2 + which) * p.Hkv + head) * kFp4Slab<D>;
+                        store_fp4<D>(slab, (int)(place % kPage), c, codes, exponent);
+                        continue;
+                    }
                     const size_t at = row_dst[min(r0 + r, rows_here - 1)] + in_page;
-                    if constexpr (F8) reinterpret_cast<uint2 *>(p.pages_w)[at] = bf16_to_codes(v[r], which ? p.v_inv : p.k_inv);
+                    if constexpr (BITS == 8) reinterpret_cast<uint2 *>(p.pages_w)[at] = bf16_to_codes(v[r], which ? p.v_inv : p.k_inv);
                     else reinterpret_cast<u32x4 *>(p.pages_w)[at] = v[r];
                 }
             }
@@ -115,7 +127,7 @@ __device__ __forceinline__ void zero_padding_rows(const AttnParams &p, int grp, 
     }
 }
 
-template <int D, int KS, bool F8>
+template <int D, int KS, int BITS>
 __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(AttnParams p)
 {
     constexpr int STAGE = Shape<KS>::STAGE;
@@ -134,7 +146,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     int abid = blockIdx.x;                           // index in the attention grid
     if (abid >= p.attn_first) {
         if (abid < p.attn_first + p.append_blocks) {
-            append_rows<D, F8>(p, reinterpret_cast<unsigned long long *>(smem), abid - p.attn_first, p.append_blocks, threadIdx.x, NT);
+            append_rows<D, BITS>(p, reinterpret_cast<unsigned long long *>(smem), abid - p.attn_first, p.append_blocks, threadIdx.x, NT);
             return;
         }
         abid -= p.append_blocks;
@@ -164,7 +176,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     const int kh = magic_div(grp, p.kv_magic);
     const int first_page = min(wave, p.max_blocks - 1), first_page_hi = min(wave + Shape<KS>::SLOTS, p.max_blocks - 1);
 
-    const WaveSrc ws = make_wave_src<D, KS, F8>(p, kh);    // for the first job's first loads; every job derives its own
+    const WaveSrc ws = make_wave_src<D, KS, BITS>(p, kh);    // for the first job's first loads; every job derives its own
 
     // ---- the workgroup's first job.  Lane l looks at segment s0 + l (64 at a time); it also fetches
     // what the owner of the job will need next (context length, the pages of the segment's first
@@ -394,7 +406,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     // first (the older wavefront of a SIMD is served first), so they issue the loads of their partner
     // in part 1 as well.
     static_assert(Shape<KS>::STAGE / kPage == Shape<KS>::WAVES, "stage 0: wavefront w loads page w of the segment");
-    Carry<D> cy;
+    Carry<D, BITS> cy;
     cy.par = J.it_begin & 1;                         // the first stage goes to buffer 0
     {
         // the job's Q rows, by way of the second stage buffer (its first loads go out behind the job's first barrier)
@@ -411,12 +423,12 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         };
         constexpr int PPS = Shape<KS>::STAGE / kPage;           // pages per stage
         cy.have_codes = false;
-        if (F8 && J.it_begin < J.src.n_ctx_tiles) {
-            // a pool of FP8 codes and a first stage of cached keys: every wavefront requests the codes of its own rows
+        if (BITS < 16 && J.it_begin < J.src.n_ctx_tiles) {
+            // a pool of codes and a first stage of cached keys: every wavefront requests the codes of its own rows
             if (J.it_begin != 0 || !pages_fetched) page = row_entry(J.it_begin * PPS + wave);
             StageLoads sl;
-            const bool full = describe_stage_loads<D, KS, F8>(J.src, ws, lo, page, J.it_begin, wave, new_row_bytes, lds_address(smem), sl);
-            fetch_stage_codes<D>(sl, full, cy.codes);
+            const bool full = describe_stage_loads<D, KS, BITS>(J.src, ws, lo, page, J.it_begin, wave, new_row_bytes, lds_address(smem), sl);
+            if constexpr (BITS < 16) fetch_stage_codes<D>(sl, full, cy.codes);
             cy.have_codes = true;
             wait_vm<0>();
         } else if (kq == 0) {
@@ -458,7 +470,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
                 --n_later;
             }
         }
-        tile_job<D, KS, F8, false>(p, first, &params, smem, Mstat, peek, old_stash, J, more, N, cy, ho);
+        tile_job<D, KS, BITS, false>(p, first, &params, smem, Mstat, peek, old_stash, J, more, N, cy, ho);
         if (!more) break;
         J = N;
     }
@@ -482,24 +494,28 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     TETRI_MARK(7);
 }
 
-template <int D, int KS, bool F8>
+template <int D, int KS, int BITS>
 hipError_t launch(const AttnParams &p, hipStream_t stream)
 {
-    hipLaunchKernelGGL((attn_tile_kernel<D, KS, F8>), dim3(p.attn_grid + p.append_blocks), dim3(Shape<KS>::WAVES * 64), 0, stream, p);
+    hipLaunchKernelGGL((attn_tile_kernel<D, KS, BITS>), dim3(p.attn_grid + p.append_blocks), dim3(Shape<KS>::WAVES * 64), 0, stream, p);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, bool fp8_pool, hipStream_t stream)
+hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, int pool_bits, hipStream_t stream)
 {
-    if (p.plan != nullptr) return tetri_launch_planned(p, fp8_pool, stream);
-    if (fp8_pool) {
-        if (h->cfg.head_dim == 128)
-            return key_parts == 2 ? launch<128, 2, true>(p, stream) : launch<128, 1, true>(p, stream);
-        return key_parts == 2 ? launch<64, 2, true>(p, stream) : launch<64, 1, true>(p, stream);
+    if (p.plan != nullptr) return pool_bits == 4 ? hipErrorInvalidValue : tetri_launch_planned(p, pool_bits == 8, stream);
+    const bool wide = h->cfg.head_dim == 128;
+    switch (pool_bits) {
+    case 4:
+        if (wide) return key_parts == 2 ? launch<128, 2, 4>(p, stream) : launch<128, 1, 4>(p, stream);
+        return key_parts == 2 ? launch<64, 2, 4>(p, stream) : launch<64, 1, 4>(p, stream);
+    case 8:
+        if (wide) return key_parts == 2 ? launch<128, 2, 8>(p, stream) : launch<128, 1, 8>(p, stream);
+        return key_parts == 2 ? launch<64, 2, 8>(p, stream) : launch<64, 1, 8>(p, stream);
+    default:
+        if (wide) return key_parts == 2 ? launch<128, 2, 16>(p, stream) : launch<128, 1, 16>(p, stream);
+        return key_parts == 2 ? launch<64, 2, 16>(p, stream) : launch<64, 1, 16>(p, stream);
     }
-    if (h->cfg.head_dim == 128)
-        return key_parts == 2 ? launch<128, 2, false>(p, stream) : launch<128, 1, false>(p, stream);
-    return key_parts == 2 ? launch<64, 2, false>(p, stream) : launch<64, 1, false>(p, stream);
 }

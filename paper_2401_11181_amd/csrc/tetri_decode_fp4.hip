@@ -1,0 +1,649 @@
+// One decode iteration over a paged cache of 4-bit codes (cache_fp4.h) for gfx950: tetri_decode.hip's counterpart.  The batch is cut the same
+// ways (a workgroup per (request, kv head), equal parts of each, or equal ranges of the whole batch's steps), partial results meet the
+// same way; what a wavefront does with its steps is another thing, because codes are a quarter of the bytes: reading them is
+// 4.25 * D / 8 bytes per cached token and kv head, and at that rate the work per byte counts.
+//
+//   * A step is 32 keys, two pages, of one (request, kv head).  A slab of 1088 bytes (D = 128) comes straight into LDS: a page's codes by one
+//     instruction, the exponents of all four slabs of the step by one more.  A wavefront has a ring of kDepth steps of its own; no
+//     barrier stands between steps.
+//   * Codes become bf16 in registers, with their power of two (v_cvt_scalef32_pk_bf16_fp4, exact), and the products are 16x16x32 bf16 ones: sums are
+//     32-bit numbers.  (The products that take such codes and their exponents as they are, v_mfma_scale_f32_16x16x128_f8f6f4, need Q in 8-bit
+//     pieces, and they sum with fewer bits: of N(0, 1) scores of 128 products they lost 4e-6 of the root mean square, with one channel 50 times as large 3e-5 and
+//     up to 0.03 of a single score; this way 1e-8.)
+//   * S^T = K Q^T: the fragment of a lane is 8 neighbouring elements of a row, in any order over the lanes as long as Q's is the same: a lane takes
+//     D / 4 neighbouring codes of one key, which share an exponent.
+//   * O^T += V^T P^T needs several keys of one d in a lane, and codes of neighbouring d share a byte.  A lane reads D / 16 neighbouring codes of each of 8
+//     keys, converts pairs of them and puts the halves of two keys together (v_perm_b32): no transposition through LDS.  Row m of the
+//     product is then d = D / 16 * m + j, j its number.
+//   * Which key is which row of a page's product is free too: row 4a + b is key 4b + a, so that the rows which a V instruction reads are neighbours.
+//   * Slots past the end of a request's cache may hold anything: their scores are masked, their exponents replaced (a code is
+//     finite, an exponent may stand for NaN).  Pages past the end are not looked up.
+//   * The new token is not quantised: its score is summed in 32 bits by the wavefront that has the request's last step.
+#include "cache_fp4.h"
+
+namespace {
+
+using namespace tetri_dev;
+
+constexpr int kMergeCols = 4;     // query heads whose partial O the merge area in LDS holds at a time
+constexpr int kWaves = 4;         // wavefronts of a workgroup
+
+// A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
+template <int D> __device__ __forceinline__ int part_floats(int g) { return g * D + ((2 * g + 3) & ~3); }
+
+__device__ __forceinline__ float load_coherent(const float *p)
+{
+    return __hip_atomic_load(reinterpret_cast<const __attribute__((address_space(1))) float *>((uintptr_t)p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_coherent2(const float *p)
+{
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const __attribute__((address_space(1))) uint64_t *>((uintptr_t)p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32)));
+}
+__device__ __forceinline__ void store_coherent2(float *p, float x, float y)
+{
+    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, x) | (uint64_t)__builtin_bit_cast(uint32_t, y) << 32;
+    __hip_atomic_store(reinterpret_cast<__attribute__((address_space(1))) uint64_t *>((uintptr_t)p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// A stretch of steps of one request; wave-uniform.  A request without a cached token has one step, without keys.
+struct Job {
+    int b;                      // request
+    int begin, end;             // steps [begin, end)
+    int L;                      // cached tokens of the request
+    __device__ __forceinline__ int steps() const { return max((L + 31) >> 5, 1); }
+};
+
+// A step in LDS: codes of K of both pages, of V of both, then the exponents of K and V of page 0 and K and V of page 1 (behind each other,
+// kScaleBytes of each; D = 128: row 4a + b of a slab's at place 4b + a).
+template <int D> struct Step {
+    static constexpr int ROW = D / 2, PAGE_BYTES = kPage * ROW, SCALE_BYTES = kPage * D / 32;
+    static constexpr int V = 2 * PAGE_BYTES, SCALES = 4 * PAGE_BYTES;
+    static constexpr int BYTES = SCALES + (D == 128 ? 256 : 256);        // (an instruction of 64 lanes of 4 bytes)
+    static constexpr int LOADS = D == 128 ? 5 : 3;                       // instructions
+    static constexpr int DEPTH = D == 128 ? 4 : 4;                       // steps a wavefront's ring holds
+};
+
+// 64 lanes of 4 bytes, lane l's from base + off to LDS byte lds + 4 * l, past the caches as dma16_stream's.
+__device__ __forceinline__ void dma4_stream(const void *p, uint32_t lds)
+{
+    lds = __builtin_amdgcn_readfirstlane(lds);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+}
+// The same of 16 bytes, every lane with an address of its own.
+__device__ __forceinline__ void dma16_stream_lanes(const void *p, uint32_t lds)
+{
+    lds = __builtin_amdgcn_readfirstlane(lds);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+}
+
+constexpr int kDecodeLead = 56;   // bytes of the kernel's arguments in front of its structure (see tetri_decode.hip)
+
+// NB: blocks of 16 query heads.  RANGES and the grid as decode_attn_kernel.
+template <int D, int NB, bool RANGES>
+__global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_t *ctx_lens, const int32_t *bt, const uint16_t *pages, int max_blocks, int Hkv,
+                                                                    uint32_t hkv_magic, int parts, const uint16_t *q, int B, DecodeArgs)
+{
+    typedef __attribute__((address_space(4))) const DecodeArgs const_decode_args;
+    typedef Step<D> T;
+    constexpr int NW = kWaves, NT = NW * 64, KS = D / 32, DJ = D / 16, DEPTH = T::DEPTH;
+    __shared__ __attribute__((aligned(1024))) char smem[NW * DEPTH * T::BYTES];
+    __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
+    __shared__ float stat[NW][2][32];
+    __shared__ int arrived;
+    const const_decode_args *p = (const const_decode_args *)((__attribute__((address_space(4))) const char *)__builtin_amdgcn_kernarg_segment_ptr() + kDecodeLead);
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = lane >> 4, l16 = lane & 15;
+    // a context length outside what the block table can describe is clamped: whatever the device arrays hold, no address is formed
+    // from a block-table index out of range
+    auto ctx_of = [&](int b) -> int { return min(max(((const const_i32 *)(uintptr_t)ctx_lens)[b], 0), max_blocks * kPage); };
+
+    const int wg = magic_div(blockIdx.x, hkv_magic), kh = blockIdx.x - wg * Hkv;
+    auto clear_next = [&]() {
+        const int n = p->n_counters;
+        for (int i = blockIdx.x * NT + tid; i < n; i += gridDim.x * NT) store_global(p->counters_next + i, 0);
+    };
+    // ---- the workgroup's first job; `left` steps of its range behind it
+    Job job;
+    int left = 0, div_q, div_r = 0, pos;
+    if constexpr (!RANGES) {
+        job.b = parts == 1 ? wg : wg / parts;
+        pos = wg - job.b * parts;
+        job.L = ctx_of(job.b);
+        div_q = parts == 1 ? job.steps() : (job.steps() + parts - 1) / parts;
+        job.begin = pos * div_q;
+        job.end = min(job.steps(), job.begin + div_q);
+        if (job.begin >= job.end) {                      // fewer steps than parts: nobody waits for this one
+            clear_next();
+            return;
+        }
+    } else {
+        // lane l looks at requests l * R .. l * R + R - 1
+        const int R = (B + 63) >> 6;
+        const int32_t *ctx = ctx_lens;
+        auto steps_of = [&](int b) -> int { return max((min(max(ctx[b], 0), max_blocks * kPage) + 31) >> 5, 1); };
+        int mine = 0;
+        for (int i = 0; i < R; ++i) {
+            const int b = lane * R + i;
+            if (b < B) mine += steps_of(b);
+        }
+        int incl = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(incl, d, 64);
+            if (lane >= d) incl += y;
+        }
+        const int total = __builtin_amdgcn_readlane(incl, 63);
+        const int ranges = min(p->ranges, (int)((uint32_t)(total + p->min_steps - 1) / (uint32_t)p->min_steps));
+        if (wg >= ranges) {
+            clear_next();
+            return;
+        }
+        div_q = __builtin_amdgcn_readfirstlane((int)((uint32_t)total / (uint32_t)ranges));
+        div_r = total - div_q * ranges;
+        pos = wg * div_q + min(wg, div_r);
+        left = div_q + (int)(wg < div_r);
+        // the request of step `pos`: its lane, then inside the lane's block
+        int base = incl - mine, found = -1, fl = 0, fbase = 0;
+        if (pos >= base && pos < incl)
+            for (int i = 0; i < R; ++i) {
+                const int b = min(lane * R + i, B - 1), n = steps_of(b);
+                if (found < 0 && pos < base + n) { found = b; fl = min(max(ctx[b], 0), max_blocks * kPage); fbase = base; }
+                base += n;
+            }
+        const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(found >= 0) | (1ull << 63));
+        job.b = __builtin_amdgcn_readlane(found, src);
+        if (job.b < 0) return;                           // (ctx_lens written to while the launch runs: no address is formed from it)
+        job.L = __builtin_amdgcn_readlane(fl, src);
+        job.begin = pos - __builtin_amdgcn_readlane(fbase, src);
+        job.end = min(job.steps(), job.begin + left);
+        left -= job.end - job.begin;
+    }
+    // the job after `j`, with `rest` steps of the range behind j: rest goes down by the new job's steps
+    auto next_job = [&](Job &j, int &rest) {
+        ++j.b;
+        j.L = ctx_of(min(j.b, B - 1));
+        j.begin = 0;
+        j.end = min(j.steps(), rest);
+        rest -= j.end;
+    };
+
+    const uint32_t page_bytes = 2 * Hkv * kFp4Slab<D>, v_delta = Hkv * kFp4Slab<D>;
+    const char *pool = reinterpret_cast<const char *>(pages) + (size_t)kh * kFp4Slab<D>;
+    char *my = smem + wave * (DEPTH * T::BYTES);
+    const uint32_t my_lds = lds_address(my);
+
+    // ---- where a lane's part of a step comes from.  K, D = 128: place (row, c) of LDS has chunk c ^ row / 4 of the row (16 bytes), so that the
+    // 16 lanes that read the same chunk of all rows meet no bank twice.
+    const uint32_t k_off = D == 128 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4)) << 4) : (lane & 31) * 16;
+    const uint32_t v_off = D == 128 ? lane * 16 : (lane & 31) * 16;
+    uint32_t s_off;                                      // ... of the slab's exponents
+    bool s_second, s_is_v;                               // ... of which page, and of V
+    if constexpr (D == 128) {
+        s_off = kFp4Codes<D> + (4 * (l16 & 3) + (l16 >> 2)) * 4;
+        s_is_v = (grp & 1) != 0;
+        s_second = grp >= 2;
+    } else {                                             // (lanes past 32 read once more what the others do)
+        s_off = kFp4Codes<D> + (lane & 7) * 4;
+        s_is_v = (lane & 8) != 0;
+        s_second = (lane & 16) != 0;
+    }
+    if (s_is_v) s_off += v_delta;
+
+    // ---- the wavefront's cursor: the step whose loads are issued next (step fs of job fj, frest steps of the range behind that job; fs < 0: there
+    // is none) and its pages
+    Job fj = job;
+    int fs = job.begin + wave, frest = left, pg0 = 0, pg1 = 0;
+    auto settle = [&]() {
+        while (fs >= fj.end) {
+            if (!RANGES || frest == 0) { fs = -1; return; }
+            next_job(fj, frest);
+            fs = wave;
+        }
+        const int n = (fj.L + kPage - 1) / kPage;        // pages of the request
+        const const_i32 *row = (const const_i32 *)(uintptr_t)(bt + (size_t)fj.b * max_blocks);
+        pg0 = 2 * fs < n ? row[2 * fs] : 0;              // (a request without a token reads page 0 of the pool, and nothing of it counts)
+        pg1 = 2 * fs + 1 < n ? row[2 * fs + 1] : pg0;
+    };
+    auto issue = [&](int place) {
+        const uint32_t lds = my_lds + place * T::BYTES;
+        const char *a = pool + (size_t)pg0 * page_bytes, *b = pool + (size_t)pg1 * page_bytes;
+        if constexpr (D == 128) {
+            const uint32_t ko[1] = {k_off}, vo[1] = {v_off};
+            dma16_stream<1>(a, ko, lds);
+            dma16_stream<1>(b, ko, lds + T::PAGE_BYTES);
+            dma4_stream((s_second ? b : a) + s_off, lds + T::SCALES);
+            dma16_stream<1>(a + v_delta, vo, lds + T::V);
+            dma16_stream<1>(b + v_delta, vo, lds + T::V + T::PAGE_BYTES);
+        } else {
+            const char *mine = lane < 32 ? a : b;
+            dma16_stream_lanes(mine + k_off, lds);
+            dma4_stream((s_second ? b : a) + s_off, lds + T::SCALES);
+            dma16_stream_lanes(mine + v_delta + v_off, lds + T::V);
+        }
+    };
+    // Q fragments (B operand of S^T): column l16 is query head kh * g + l16 of the block, zero past g; element 8 s .. of a lane's D / 4 ones
+    bf16x8 qf[NB][KS];
+    auto load_q = [&](int b) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int g = p->g;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int col = 16 * nb + (ln & 15);
+            const global_u32x4 *qp = reinterpret_cast<const global_u32x4 *>((uintptr_t)(q + ((size_t)b * p->Hq + (size_t)kh * g + min(col, g - 1)) * D + (ln >> 4) * (D / 4)));
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                u32x4 v = u32x4(qp[s]);
+                if (col >= g) v = u32x4{0u, 0u, 0u, 0u};
+                qf[nb][s] = __builtin_bit_cast(bf16x8, v);
+            }
+        }
+    };
+
+    // ---- the first loads.  The steps in flight are remembered in order: c* the current one, then what follows it
+    int ahead = 0;                                       // steps in flight, the current one included
+    int rb[DEPTH], rs[DEPTH], rL[DEPTH];                 // (a shift register: request, step and length of each)
+    int place_in = 0, place_out = 0;
+    settle();
+    const bool any = fs >= 0;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) {
+        rb[i] = 0; rs[i] = -1; rL[i] = 0;
+        if (fs >= 0) {
+            issue(place_in);
+            if (++place_in == DEPTH) place_in = 0;
+            rb[i] = fj.b; rs[i] = fs; rL[i] = fj.L;
+            ++ahead;
+            if (i == 0) load_q(fj.b);
+            fs += NW;
+            settle();
+        }
+    }
+    (void)any;
+
+    const float c = p->neg ? -p->c : p->c;
+
+    for (;;) {                                           // the jobs of the range
+    f32x4 o[NB][DJ];
+    float m[NB], lsum[NB];                               // m: a reference exponent, not the exact maximum
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        m[nb] = -1e30f;
+        lsum[nb] = 0.f;
+#pragma unroll
+        for (int j = 0; j < DJ; ++j) o[nb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    while (rs[0] >= 0 && (!RANGES || rb[0] == job.b)) {
+        const int cb = rb[0], cs = rs[0], cL = rL[0];
+        const bool last = cs + 1 == max((cL + 31) >> 5, 1);          // the request's last step
+        // the step has landed when only what was issued after it is outstanding
+        switch (ahead) {
+        case 1: wait_vm<0>(); break;
+        case 2: wait_vm<T::LOADS>(); break;
+        case 3: wait_vm<2 * T::LOADS>(); break;
+        default: wait_vm<3 * T::LOADS>(); break;
+        }
+        static_assert(DEPTH == 4, "waits for up to three steps behind the current one");
+        const char *tile = my + place_out * T::BYTES;
+        // ---- scores
+        f32x4 sc[NB][2];
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+            const int row = 4 * (l16 & 3) + (l16 >> 2);
+            uint32_t kw[KS], e;
+            if constexpr (D == 128) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + pg * T::PAGE_BYTES + row * 64 + ((grp ^ (row >> 2)) << 4));
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kw[s] = x[s];
+                e = *reinterpret_cast<const uint8_t *>(tile + T::SCALES + pg * (2 * T::SCALE_BYTES) + 4 * l16 + grp);
+            } else {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(tile + pg * T::PAGE_BYTES + row * 32 + grp * 8);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kw[s] = x[s];
+                e = *reinterpret_cast<const uint8_t *>(tile + T::SCALES + pg * (2 * T::SCALE_BYTES) + 2 * row + (grp >> 1));
+            }
+            const float scale = fp4_scale(e);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_to_bf16(kw[s], scale));
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nb][s], sc[nb][pg], 0, 0, 0);
+            }
+        }
+        // ---- V's codes and exponents: key 4i + grp of both pages
+        uint32_t vw[8];
+        float vs[8];
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+            const char *v = tile + T::V + pg * T::PAGE_BYTES, *es = tile + T::SCALES + (2 * pg + 1) * T::SCALE_BYTES;
+            if constexpr (D == 128) {
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(es + 16 * grp);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    vw[4 * pg + i] = *reinterpret_cast<const uint32_t *>(v + (4 * i + grp) * 64 + l16 * 4);
+                    vs[4 * pg + i] = fp4_scale((w[i] >> (8 * (l16 >> 2))) & 255u);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    vw[4 * pg + i] = *reinterpret_cast<const uint16_t *>(v + (4 * i + grp) * 32 + l16 * 2);
+                    vs[4 * pg + i] = fp4_scale(*reinterpret_cast<const uint8_t *>(es + 2 * (4 * i + grp) + (l16 >> 3)));
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // everything is in registers: the place may be overwritten
+        const bool far = fs >= 0;
+        if (far) issue(place_in);
+        if (++place_out == DEPTH) place_out = 0;
+        // ---- scores in units of log2, slots past the end masked
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[nb][pg][i] *= c;
+        if (last) {
+            const int n = cL - 32 * cs;                              // keys of the step
+#pragma unroll
+            for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * pg + 4 * i + grp >= n) {
+                        vs[4 * pg + i] = 0.f;
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) sc[nb][pg][i] = -INFINITY;
+                    }
+        }
+        bf16x8 pf[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            // m stays as it is unless a score exceeds it by 8 (weights are floating-point numbers: no precision is lost below)
+            float top = -INFINITY;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) top = fmaxf(top, sc[nb][x / 4][x % 4]);
+            if (__builtin_amdgcn_ballot_w64(top > m[nb] + 8.f) != 0) {
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(m[nb], top), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new);
+                m[nb] = m_new;
+                lsum[nb] *= alpha;
+#pragma unroll
+                for (int j = 0; j < DJ; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nb][j][i] *= alpha;
+            }
+            // weights, rounded to bf16 for the PV product; the row sum is of the rounded ones
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                pf[nb][x] = (__bf16)__builtin_amdgcn_exp2f(sc[nb][x / 4][x % 4] - m[nb]);
+                lsum[nb] += (float)pf[nb][x];
+            }
+        }
+        // ---- O^T += V^T P^T
+#pragma unroll
+        for (int t = 0; t < DJ / 2; ++t) {
+            uint32_t x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                bf16x2 y;
+                if (t == 0) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 0);
+                else if (t == 1) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 1);
+                else if (t == 2) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 2);
+                else y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 3);
+                x[k] = __builtin_bit_cast(uint32_t, y);
+            }
+            u32x4 even, odd;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                even[k] = __builtin_amdgcn_perm(x[2 * k + 1], x[2 * k], 0x05040100u);
+                odd[k] = __builtin_amdgcn_perm(x[2 * k + 1], x[2 * k], 0x07060302u);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                o[nb][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pf[nb], o[nb][2 * t], 0, 0, 0);
+                o[nb][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pf[nb], o[nb][2 * t + 1], 0, 0, 0);
+            }
+        }
+        if (last) {
+            // the new token: a lane has D / 4 products of its score, and the rows of O that it holds
+            const size_t at = ((size_t)cb * Hkv + kh) * D;
+            const global_u32x4 *kp = reinterpret_cast<const global_u32x4 *>((uintptr_t)(p->k_new + at + grp * (D / 4)));
+            u32x4 kn[KS], vn[4];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kn[s] = u32x4(kp[s]);
+            // row 4 * grp + i of the products is d = DJ * (4 * grp + i) ..: DJ bf16 of v_new
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint16_t *src = p->v_new + at + DJ * (4 * grp + i);
+                if constexpr (DJ == 8) {
+                    vn[i] = *reinterpret_cast<global_u32x4 *>((uintptr_t)src);
+                } else {
+                    const u32x2 y = *reinterpret_cast<__attribute__((address_space(1))) const u32x2 *>((uintptr_t)src);
+                    vn[i] = u32x4{y[0], y[1], 0u, 0u};
+                }
+            }
+            auto value = [](const u32x4 &w, int j) -> float { return __builtin_bit_cast(float, (j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16); };
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float s = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(value(kn[k], j), value(__builtin_bit_cast(u32x4, qf[nb][k]), j), s);
+                s += __shfl_xor(s, 16, 64);
+                s += __shfl_xor(s, 32, 64);
+                s *= c;
+                const float m_new = fmaxf(m[nb], s), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
+                m[nb] = m_new;
+                lsum[nb] = lsum[nb] * alpha + (grp == 0 ? w : 0.f);
+#pragma unroll
+                for (int j = 0; j < DJ; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nb][j][i] = __builtin_fmaf(w, value(vn[i], j), o[nb][j][i] * alpha);
+            }
+        }
+        // on to the next step (its Q rows, if it is another request's, are requested here)
+#pragma unroll
+        for (int i = 0; i + 1 < DEPTH; ++i) { rb[i] = rb[i + 1]; rs[i] = rs[i + 1]; rL[i] = rL[i + 1]; }
+        rs[DEPTH - 1] = -1;
+        --ahead;
+        if (far) {
+            rb[DEPTH - 1] = fj.b; rs[DEPTH - 1] = fs; rL[DEPTH - 1] = fj.L;
+            ++ahead;
+            if (++place_in == DEPTH) place_in = 0;
+            fs += NW;
+            settle();
+        }
+        if (RANGES && rs[0] >= 0 && rb[0] != cb) load_q(rb[0]);
+    }
+
+    // ---- the job is done: the wavefronts merge.  (The tiles may be receiving the next job's first steps: the merge has an area of its own in
+    // LDS, for kMergeCols query heads at a time.)
+    const const_decode_args *e = p;
+    int te = tid;
+    asm volatile("" : "+v"(te), "+s"(e));                // (values worked out and read here, not kept across the loop)
+    const int grp_e = (te >> 4) & 3, l16_e = te & 15, g = e->g;
+    const bool ends = job.end == job.steps(), whole = ends && job.begin == 0;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        float l = lsum[nb];
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (grp_e == 0) { stat[wave][0][16 * nb + l16_e] = m[nb]; stat[wave][1][16 * nb + l16_e] = l; }
+    }
+    if (ends && e->pages_w != nullptr && job.L < max_blocks * kPage && wave == NW - 1 && (te & 63) < D / 4) {
+        // fused append: the codes of the new token's K and V row of this kv head go to slot L % 16 of page block_table[b][L / 16], 8
+        // values a lane (nothing that counts in this launch reads that slot: key L comes from k_new / v_new everywhere)
+        constexpr int LR = D / 8;                            // lanes of a row
+        const int which = (te & 63) / LR, chunk = te % LR;
+        const int page = ((const const_i32 *)(uintptr_t)(bt + (size_t)job.b * max_blocks))[job.L / kPage];
+        const uint16_t *src = (which ? e->v_new : e->k_new) + ((size_t)job.b * Hkv + kh) * D + chunk * 8;
+        uint32_t exponent;
+        const uint32_t codes = bf16_to_fp4(u32x4(*reinterpret_cast<global_u32x4 *>((uintptr_t)src)), exponent);
+        char *slab = reinterpret_cast<char *>(e->pages_w) + (size_t)page * page_bytes + (which ? v_delta : 0) + (size_t)kh * kFp4Slab<D>;
+        store_fp4<D>(slab, job.L % kPage, chunk, codes, exponent);
+    }
+    // a request cut between workgroups: which part of how many this is, and where the parts are (a workgroup keeps the first part of a
+    // request in its second place, any other part in its first one: it has at most one of each)
+    int piece = 0, pieces = 1, w0 = 0, counter = 0;
+    if (!whole) {
+        if constexpr (!RANGES) {
+            piece = pos;
+            pieces = (job.steps() + div_q - 1) / div_q;
+            w0 = wg - piece;
+            counter = job.b;
+        } else {
+            auto owner = [&](int x) -> int {             // the range that has step x of the sequence
+                const int cut = div_r * (div_q + 1);
+                return __builtin_amdgcn_readfirstlane(x < cut ? (int)((uint32_t)x / (uint32_t)(div_q + 1)) : div_r + (int)((uint32_t)(x - cut) / (uint32_t)div_q));
+            };
+            w0 = owner(pos - job.begin);                 // pos: the sequence position of the job's first step
+            pieces = owner(pos - job.begin + job.steps() - 1) - w0 + 1;
+            piece = wg - w0;
+            counter = w0;
+        }
+        counter = counter * Hkv + kh;
+    }
+    const int pfl = part_floats<D>(g);
+    float *partial = e->partial;
+    auto place = [&](int i) -> float * { return partial + ((size_t)(RANGES ? 2 * (w0 + i) + (int)(i == 0) : w0 + i) * Hkv + kh) * pfl; };
+    const size_t head = (size_t)job.b * e->Hq + (size_t)kh * g;
+    uint16_t *out = e->out;
+    auto write_pair = [&](size_t at, float x, float y, float l) {
+        const float inv = 1.0f / l;
+        bf16x2 r;
+        r[0] = (__bf16)(x * inv);
+        r[1] = (__bf16)(y * inv);
+        *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)(out + at)) = __builtin_bit_cast(uint32_t, r);
+    };
+    for (int c0 = 0; c0 < g; c0 += kMergeCols) {
+        if (c0 != 0) lds_barrier();                      // everybody is done with the columns before
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int col = 16 * nb + l16_e;
+            if (col >= c0 && col < min(g, c0 + kMergeCols)) {
+                float *mine = area[wave][col - c0];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < DJ; j += 4)
+                        *reinterpret_cast<f32x4 *>(mine + DJ * (4 * grp_e + i) + j) = f32x4{o[nb][j][i], o[nb][j + 1][i], o[nb][j + 2][i], o[nb][j + 3][i]};
+            }
+        }
+        lds_barrier();
+        // two neighbouring values of one head per thread
+        for (int v = te; v < min(g - c0, kMergeCols) * (D / 2); v += NT) {
+            const int cc = v / (D / 2), col = c0 + cc, d = 2 * (v - cc * (D / 2));
+            float ms = stat[0][0][col];
+#pragma unroll
+            for (int i = 1; i < NW; ++i) ms = fmaxf(ms, stat[i][0][col]);
+            float x = 0.f, y = 0.f, l = 0.f;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) {
+                const float wgt = __builtin_amdgcn_exp2f(stat[i][0][col] - ms);
+                const float2 z = *reinterpret_cast<const float2 *>(&area[i][cc][d]);
+                x = __builtin_fmaf(z.x, wgt, x);
+                y = __builtin_fmaf(z.y, wgt, y);
+                l = __builtin_fmaf(stat[i][1][col], wgt, l);
+            }
+            if (whole) {
+                write_pair((head + col) * D + d, x, y, l);
+            } else {
+                float *mine = place(piece);
+                store_coherent2(mine + col * D + d, x, y);
+                if (d == 0) {
+                    store_coherent(mine + g * D + col, ms);
+                    store_coherent(mine + g * D + g + col, l);
+                }
+            }
+        }
+    }
+    if (!whole) {
+        coherent_stores_done();
+        lds_barrier();
+        if (te == 0) arrived = atomic_add_global(e->counters + counter, 1);
+        lds_barrier();
+        if (__builtin_amdgcn_readfirstlane(arrived) == pieces - 1) {
+            // all the others have been here: the counter goes back to zero, the parts are merged in their order.  With few columns the
+            // threads form groups that take every groups-th part, and the groups meet in LDS.
+            if (te == 0) store_global(e->counters + counter, 0);
+            const int pairs = g * (D / 2), groups = max(1, NT / pairs);
+            for (int v0 = 0; v0 < pairs; v0 += NT) {
+                const int grp_m = groups > 1 ? te / pairs : 0, v = groups > 1 ? te - grp_m * pairs : v0 + te;
+                const bool on = grp_m < groups && v < pairs;
+                const int col = v / (D / 2);
+                float mm = -INFINITY, l = 0.f, x = 0.f, y = 0.f;
+                if (on)
+                    for (int i0 = grp_m; i0 < pieces; i0 += 8 * groups) {
+                        float mi[8], li[8];
+                        float2 xi[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float *src = place(min(i0 + i * groups, pieces - 1));
+                            mi[i] = load_coherent(src + g * D + col);
+                            li[i] = load_coherent(src + g * D + g + col);
+                            xi[i] = load_coherent2(src + 2 * v);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (i0 + i * groups < pieces) {
+                                const float m_new = fmaxf(mm, mi[i]);
+                                const float w_old = __builtin_amdgcn_exp2f(mm - m_new), w_new = __builtin_amdgcn_exp2f(mi[i] - m_new);
+                                mm = m_new;
+                                l = __builtin_fmaf(li[i], w_new, l * w_old);
+                                x = __builtin_fmaf(xi[i].x, w_new, x * w_old);
+                                y = __builtin_fmaf(xi[i].y, w_new, y * w_old);
+                            }
+                    }
+                if (groups > 1) {
+                    // (a group without a part has m = -inf and weighs nothing; group 0 always has one)
+                    float *meet = &area[0][0][0];
+                    static_assert(NW * kMergeCols * D >= 4 * NT, "four floats per thread");
+                    if (on) *reinterpret_cast<f32x4 *>(meet + 4 * te) = f32x4{mm, l, x, y};
+                    lds_barrier();
+                    if (on && grp_m == 0)
+                        for (int i = 1; i < groups; ++i) {
+                            const f32x4 z = *reinterpret_cast<const f32x4 *>(meet + 4 * (i * pairs + v));
+                            const float m_new = fmaxf(mm, z[0]);
+                            const float w_old = __builtin_amdgcn_exp2f(mm - m_new), w_new = __builtin_amdgcn_exp2f(z[0] - m_new);
+                            mm = m_new;
+                            l = __builtin_fmaf(z[1], w_new, l * w_old);
+                            x = __builtin_fmaf(z[2], w_new, x * w_old);
+                            y = __builtin_fmaf(z[3], w_new, y * w_old);
+                        }
+                }
+                if (on && grp_m == 0) write_pair(head * D + 2 * v, x, y, l);
+            }
+        }
+    }
+    if (!RANGES || left == 0) break;
+    pos += job.end - job.begin;
+    next_job(job, left);
+    lds_barrier();                                       // everybody is done with stat, area and `arrived`
+    }
+    clear_next();
+}
+
+template <int D, int NB> hipError_t launch(const DecodeParams &p, hipStream_t stream)
+{
+    const dim3 grid((p.parts > 0 ? p.B * p.parts : p.ranges) * p.Hkv);
+    auto kernel = p.parts > 0 ? decode_fp4_kernel<D, NB, false> : decode_fp4_kernel<D, NB, true>;
+    static_assert(KernelArgs<decltype(kernel)>::last_offset() == kDecodeLead, "where the kernel reads its structure");
+    hipLaunchKernelGGL(kernel, grid, dim3(kWaves * 64), 0, stream, p.ctx, p.bt, p.pages, p.max_blocks, p.Hkv, p.hkv_magic, p.parts, p.q, p.B,
+                       static_cast<const DecodeArgs &>(p));
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t tetri_launch_decode_fp4(const tetri_ctx *h, const DecodeParams &p, hipStream_t stream)
+{
+    if (p.g > 32) return hipErrorInvalidValue;
+    if (h->cfg.head_dim == 128) return p.g > 16 ? launch<128, 2>(p, stream) : launch<128, 1>(p, stream);
+    return p.g > 16 ? launch<64, 2>(p, stream) : launch<64, 1>(p, stream);
+}

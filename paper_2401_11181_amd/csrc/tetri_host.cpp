@@ -216,7 +216,7 @@ tetri_status tetri_kv_append(tetri_ctx *h, const void *k_new, const void *v_new,
 }
 
 // mode 0: 16-bit pool <-> 16-bit buffer; 1: 16-bit pool -> buffer of FP8 codes (quantising);
-// 2: FP8 pool <-> buffer of FP8 codes (bytes)
+// 2: FP8 pool <-> buffer of FP8 codes (bytes); 3: 16-bit pool -> buffer of 4-bit codes; 4: such a buffer -> pool of them
 static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, void *buf, const int32_t *block_table,
                                 const int32_t *cu_tokens, const int32_t *first_tokens, int32_t num_reqs,
                                 int64_t total_tokens, bool to_pool, void *stream, int mode = 0, float k_scale = 1.f,
@@ -235,7 +235,7 @@ static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, vo
     if (mode == 1 && !(std::isfinite(k_scale) && std::isfinite(v_scale) && k_scale > 0.f && v_scale > 0.f))
         return fail(h, TETRI_ERR_INVALID_ARG, "%s: k_scale and v_scale must be positive and finite", fn);
     // 16-bit units of a row as the kernel moves it: an FP8 row of head_dim codes is head_dim / 2 units
-    const int32_t row_units = mode == 2 ? h->cfg.head_dim / 2 : h->cfg.head_dim;
+    const int32_t row_units = mode == 2 ? h->cfg.head_dim / 2 : (mode == 4 ? h->cfg.head_dim / 4 : h->cfg.head_dim);
     const int64_t tile_tokens = 2048 / row_units;           // a workgroup's tile: 256 lanes of 16 bytes per slab
     const int64_t tiles = total_tokens / tile_tokens + num_reqs;     // >= sum of ceil(n_r / tile_tokens)
     if (tiles > 0x7fffffff) return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many tokens for one launch", fn);
@@ -253,7 +253,7 @@ static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, vo
     // at a time closer together and leave no half-empty last round: 20000 tokens of 40x128 with 40 slabs each 203 us, with
     // 2 and 4 191.
     const int64_t slabs = 2 * (int64_t)p.Hkv;
-    p.slabs_per_wg = tiles * slabs <= 8 * (int64_t)std::max(h->num_cus, 1) ? 1 : (mode == 1 ? 4 : 2);
+    p.slabs_per_wg = tiles * slabs <= 8 * (int64_t)std::max(h->num_cus, 1) ? 1 : (mode == 1 || mode == 3 ? 4 : 2);
     if (h->transfer_slabs > 0) p.slabs_per_wg = h->transfer_slabs;
     p.slabs_per_wg = (int32_t)std::min<int64_t>(slabs, p.slabs_per_wg);
     p.slab_groups = (int32_t)((slabs + p.slabs_per_wg - 1) / p.slabs_per_wg);
@@ -262,6 +262,8 @@ static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, vo
         return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many tokens for one launch", fn);
     p.k_inv = 1.0f / k_scale; p.v_inv = 1.0f / v_scale;
     hipError_t e = mode == 1 ? tetri_launch_kv_export_fp8(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
+                 : mode == 3 ? tetri_launch_kv_export_fp4(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
+                 : mode == 4 ? tetri_launch_kv_import_fp4(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
                              : tetri_launch_kv_transfer(h, p, row_units, (int32_t)tiles, to_pool, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return TETRI_OK;
@@ -283,6 +285,21 @@ tetri_status tetri_kv_import_fp8(tetri_ctx *h, const void *buf, const int32_t *b
                        first_tokens, num_reqs, total_tokens, true, stream, 2);
 }
 
+tetri_status tetri_kv_export_fp4(tetri_ctx *h, const void *kv_pages, const int32_t *block_table, const int32_t *cu_tokens,
+                                 const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *buf, void *stream)
+{
+    return kv_transfer("tetri_kv_export_fp4", h, const_cast<void *>(kv_pages), buf, block_table, cu_tokens, first_tokens,
+                       num_reqs, total_tokens, false, stream, 3);
+}
+
+tetri_status tetri_kv_import_fp4(tetri_ctx *h, const void *buf, const int32_t *block_table, const int32_t *cu_tokens,
+                                 const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *kv_pages_fp4,
+                                 void *stream)
+{
+    return kv_transfer("tetri_kv_import_fp4", h, kv_pages_fp4, const_cast<void *>(buf), block_table, cu_tokens,
+                       first_tokens, num_reqs, total_tokens, true, stream, 4);
+}
+
 tetri_status tetri_kv_export(tetri_ctx *h, const void *kv_pages, const int32_t *block_table, const int32_t *cu_tokens,
                              const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *buf, void *stream)
 {
@@ -301,7 +318,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
                                   const void *kv_pages, void *kv_pages_w, const int32_t *block_table,
                                   const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
                                   void *stream, bool fp8 = false, float k_scale = 1.f, float v_scale = 1.f,
-                                  bool static_scratch = false, const DecodeWeights *weights = nullptr)
+                                  bool static_scratch = false, const DecodeWeights *weights = nullptr, bool fp4 = false)
 {
     if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
     const void *ptrs[] = {q, k_new, v_new, kv_pages, out};
@@ -366,7 +383,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     p.ranges = 0;
     p.min_steps = h->decode_ranges > 0 ? 1 : 4;
     const bool divisible = num_reqs <= kDecodeLookup && num_reqs * ((int64_t)cfg.max_blocks_per_seq * cfg.page_size / 32 + 1) <= 0x7fffffff;
-    const int64_t most_bytes = pairs * steps * 32 * 2 * cfg.head_dim * (fp8 ? 1 : 2);
+    const int64_t most_bytes = pairs * steps * (fp4 ? 2 * 32 * (cfg.head_dim / 2 + cfg.head_dim / 32) : 32 * 2 * cfg.head_dim * (fp8 ? 1 : 2));
     int64_t parts = h->decode_parts;
     if (parts == 0) {
         parts = std::max<int64_t>(1, std::min(2 * cus / pairs, std::min<int64_t>((steps + 2) / 3, 32)));
@@ -396,7 +413,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     p.weights_w = weights ? weights->weights_w : nullptr;
     p.score_stride = weights ? weights->score_stride : 0;
     p.max_ctx = weights ? weights->max_ctx : 0;
-    hipError_t e = tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
+    hipError_t e = fp4 ? tetri_launch_decode_fp4(h, p, static_cast<hipStream_t>(stream)) : tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares && !static_scratch) ++h->counter_turn;
     return TETRI_OK;
@@ -426,6 +443,15 @@ tetri_status tetri_decode_attn_fp8(tetri_ctx *h, const void *q, const void *k_ne
     if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_decode_attn_fp8: append must be 0 or 1");
     return decode_common("tetri_decode_attn_fp8", h, q, k_new, v_new, kv_pages_fp8, append ? kv_pages_fp8 : nullptr,
                          block_table, ctx_lens, num_reqs, max_ctx_len, scale, out, stream, true, k_scale, v_scale);
+}
+
+tetri_status tetri_decode_attn_fp4(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages_fp4, const int32_t *block_table,
+                                   const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, int32_t append, void *out,
+                                   void *stream)
+{
+    if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_decode_attn_fp4: append must be 0 or 1");
+    return decode_common("tetri_decode_attn_fp4", h, q, k_new, v_new, kv_pages_fp4, append ? kv_pages_fp4 : nullptr, block_table, ctx_lens,
+                         num_reqs, max_ctx_len, scale, out, stream, false, 1.f, 1.f, false, nullptr, true);
 }
 
 tetri_status tetri_decode_attn_append(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages,
@@ -943,7 +969,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
                                 const int32_t *ctx_lens, int32_t num_segs, float scale, void *out, void *stream,
                                 bool fp8 = false, float k_scale = 1.f, float v_scale = 1.f,
                                 const int32_t *host_cu = nullptr, const int32_t *host_ctx = nullptr, MetaUpload *carry = nullptr,
-                                const NextRows *next = nullptr)
+                                const NextRows *next = nullptr, bool fp4 = false)
 {
     const void *ptrs[] = {q, k_new, v_new, kv_pages, out};
     const char *names[] = {"q", "k_new", "v_new", "kv_pages", "out"};
@@ -1054,7 +1080,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
             p.counters = cs.use;
             p.counters_next = cs.clear;
             plan.done = plan.places != 0 && mem == 1 ? h->plan_done : nullptr;
-            hipError_t e = tetri_launch_attn(h, p, 2, fp8, hs);
+            hipError_t e = tetri_launch_attn(h, p, 2, fp8 ? 8 : 16, hs);
             if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
             if (plan.places != 0) plan_memory_used(h, mem, hs);
             return TETRI_OK;
@@ -1137,7 +1163,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
     p.kv_magic = magic((uint32_t)(p.g / p.hpw));
     if ((uint64_t)p.attn_grid * (uint64_t)(p.tiles + G + 1) >= 0x100000000ull)
         return fail(h, TETRI_ERR_UNSUPPORTED, "%s: chunk_size x heads too large for one launch", fn);
-    hipError_t e = tetri_launch_attn(h, p, key_parts, fp8, hs);
+    hipError_t e = tetri_launch_attn(h, p, key_parts, fp4 ? 4 : (fp8 ? 8 : 16), hs);
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares) {
         ++h->counter_turn;
@@ -1171,6 +1197,79 @@ tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *h, const void *q, const voi
     if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_chunk_prefill_attn_fp8: append must be 0 or 1");
     return attn_common("tetri_chunk_prefill_attn_fp8", h, q, k_new, v_new, kv_pages_fp8, append ? kv_pages_fp8 : nullptr,
                        block_table, cu, ctx_lens, num_segs, scale, out, stream, true, k_scale, v_scale);
+}
+
+tetri_status tetri_chunk_prefill_attn_fp4(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages_fp4,
+                                          const int32_t *block_table, const int32_t *cu, const int32_t *ctx_lens, int32_t num_segs, float scale,
+                                          int32_t append, void *out, void *stream)
+{
+    if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_chunk_prefill_attn_fp4: append must be 0 or 1");
+    return attn_common("tetri_chunk_prefill_attn_fp4", h, q, k_new, v_new, kv_pages_fp4, append ? kv_pages_fp4 : nullptr, block_table, cu, ctx_lens,
+                       num_segs, scale, out, stream, false, 1.f, 1.f, nullptr, nullptr, nullptr, nullptr, true);
+}
+
+tetri_status tetri_qk_norm_rope(tetri_ctx *h, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_weight,
+                                const void *k_weight, float eps, const tetri_rope *rope, const int32_t *positions, const int32_t *cu,
+                                const int32_t *ctx_lens, int32_t num_segs, int32_t num_rows, void *q_out, void *k_out, void *stream)
+{
+    const char *fn = "tetri_qk_norm_rope";
+    if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
+    const void *ptrs[] = {q, k, q_out, k_out};
+    const char *names[] = {"q", "k", "q_out", "k_out"};
+    for (int i = 0; i < 4; ++i) {
+        if (!ptrs[i]) return fail(h, TETRI_ERR_INVALID_ARG, "%s: %s is null", fn, names[i]);
+        if (!aligned16(ptrs[i])) return fail(h, TETRI_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", fn, names[i]);
+    }
+    if (!aligned16(q_weight) || !aligned16(k_weight)) return fail(h, TETRI_ERR_INVALID_ARG, "%s: q_weight or k_weight is not 16-byte aligned", fn);
+    const tetri_config &cfg = h->cfg;
+    const int64_t q_row = (int64_t)cfg.num_q_heads * cfg.head_dim, k_row = (int64_t)cfg.num_kv_heads * cfg.head_dim;
+    if (q_stride < q_row || k_stride < k_row || q_stride % 8 != 0 || k_stride % 8 != 0 || q_stride > (1ll << 40) || k_stride > (1ll << 40))
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: q_stride=%lld and k_stride=%lld have to be multiples of 8, at least %lld and %lld", fn,
+                    (long long)q_stride, (long long)k_stride, (long long)q_row, (long long)k_row);
+    if ((q_out == q && q_stride != q_row) || (k_out == k && k_stride != k_row))
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: in place only where the rows follow each other", fn);
+    if (!(std::isfinite(eps) && eps >= 0.f)) return fail(h, TETRI_ERR_INVALID_ARG, "%s: eps is negative or not finite", fn);
+    if (!rope) return fail(h, TETRI_ERR_INVALID_ARG, "%s: rope is null", fn);
+    if (rope->num_pairs < 8 || rope->num_pairs > cfg.head_dim / 2 || rope->num_pairs % 8 != 0)
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_pairs=%d is no multiple of 8 in 8..%d", fn, rope->num_pairs, cfg.head_dim / 2);
+    if (rope->num_axes < 1 || rope->num_axes > 8) return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_axes=%d outside 1..8", fn, rope->num_axes);
+    if (rope->adjacent != 0 && rope->adjacent != 1) return fail(h, TETRI_ERR_INVALID_ARG, "%s: adjacent must be 0 or 1", fn);
+    if (num_rows < 1) return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_rows=%d is not positive", fn, num_rows);
+    if (positions ? (cu || ctx_lens) : !(cu && ctx_lens))
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: either positions or cu_chunk_q_lens and ctx_lens", fn);
+    if (cu && (num_segs < 1 || num_segs > cfg.max_segs_per_chunk))
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_segs=%d outside 1..%d", fn, num_segs, cfg.max_segs_per_chunk);
+    RopeParams p;
+    for (int i = 0; i < TETRI_ROPE_PAIRS; ++i) {
+        const bool used = i < rope->num_pairs;
+        p.freq[i] = used ? rope->freq[i] : 0.f;
+        p.axis[i] = used ? rope->axis[i] : 0;
+        if (!std::isfinite(p.freq[i])) return fail(h, TETRI_ERR_INVALID_ARG, "%s: freq[%d] is not finite", fn, i);
+        if (p.axis[i] >= rope->num_axes) return fail(h, TETRI_ERR_INVALID_ARG, "%s: axis[%d]=%d of %d axes", fn, i, p.axis[i], rope->num_axes);
+    }
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != h->device)
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: the handle was created on device %d, the current device is %d", fn, h->device, dev);
+    p.q = static_cast<const uint16_t *>(q); p.k = static_cast<const uint16_t *>(k);
+    p.q_weight = static_cast<const uint16_t *>(q_weight); p.k_weight = static_cast<const uint16_t *>(k_weight);
+    p.q_out = static_cast<uint16_t *>(q_out); p.k_out = static_cast<uint16_t *>(k_out);
+    p.pos = positions; p.cu = cu; p.ctx = ctx_lens;
+    p.q_stride = q_stride; p.k_stride = k_stride;
+    p.eps = eps;
+    p.S = num_segs; p.rows = num_rows; p.Hq = cfg.num_q_heads; p.Hkv = cfg.num_kv_heads;
+    p.pairs = rope->num_pairs; p.adjacent = rope->adjacent;
+    // A row's heads go to one wavefront where rows are many (its cosines and sines are worked out once), otherwise to as many as fill eight places of
+    // a compute unit, down to the heads of one instruction each.
+    const int64_t per_inst = 512 / cfg.head_dim, insts = (p.Hq + p.Hkv + per_inst - 1) / per_inst;
+    const int64_t want = std::max<int64_t>(1, std::min(insts, 8 * (int64_t)std::max(h->num_cus, 1) / num_rows));
+    p.per_split = (int32_t)((insts + want - 1) / want);
+    p.splits = (int32_t)((insts + p.per_split - 1) / p.per_split);
+    p.splits_magic = p.splits <= 1 ? 0u : (uint32_t)((0x100000000ull + p.splits - 1) / p.splits);
+    if ((uint64_t)num_rows * p.splits * p.splits + 4ull * p.splits >= 0x7fffffffull)
+        return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many rows for one launch", fn);
+    hipError_t e = tetri_launch_rope(cfg.head_dim, p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+    return TETRI_OK;
 }
 
 // Host copies of a chunk's metadata: are they a chunk of this handle?

@@ -355,12 +355,36 @@ struct CompactParams {
     int32_t B, Hkv, max_blocks, keep, recent;
 };
 
-hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, bool fp8_pool, hipStream_t stream);
+// Norm and rotation of queries and keys (tetri_rope.hip).
+struct RopeParams {
+    const uint16_t *q, *k;            // rows of q_stride and k_stride elements
+    const uint16_t *q_weight, *k_weight;    // of the norm (null: none)
+    uint16_t *q_out, *k_out;          // [row][head][head_dim]
+    const int32_t *pos;               // [axis][row], or null:
+    const int32_t *cu, *ctx;          // the segments of a chunk
+    int64_t q_stride, k_stride;
+    float eps;
+    int32_t S, rows, Hq, Hkv;
+    int32_t pairs, adjacent;
+    int32_t splits;                   // wavefronts of a row, each of per_split instructions' heads
+    uint32_t splits_magic;            // ceil(2^32 / splits), 0 for 1
+    int32_t per_split;
+    float freq[TETRI_ROPE_PAIRS];
+    uint8_t axis[TETRI_ROPE_PAIRS];
+};
+
+// pool_bits: of an element of the pool, 16, 8 (E4M3 codes) or 4 (microscaled E2M1 codes; not for p.plan)
+hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, int pool_bits, hipStream_t stream);
 hipError_t tetri_launch_planned(const AttnParams &p, bool fp8_pool, hipStream_t stream);      // (tetri_launch_attn's, for p.plan)
 hipError_t tetri_launch_short(int head_dim, bool fp8_pool, const ShortParams &p, int wavefronts, hipStream_t stream);
 hipError_t tetri_launch_kv_transfer(const tetri_ctx *h, const TransferParams &p, int32_t row_units, int32_t tiles,
                                     bool to_pool, hipStream_t stream);
 hipError_t tetri_launch_kv_export_fp8(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);
+// The same over a pool of 4-bit codes (tetri_decode_fp4.hip).
+hipError_t tetri_launch_decode_fp4(const tetri_ctx *h, const DecodeParams &p, hipStream_t stream);
+hipError_t tetri_launch_rope(int head_dim, const RopeParams &p, hipStream_t stream);
+hipError_t tetri_launch_kv_export_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);
+hipError_t tetri_launch_kv_import_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);
 hipError_t tetri_launch_decode(const tetri_ctx *h, const DecodeParams &p, hipStream_t stream);
 // Device addresses (on the current device) of the static memory of tetri_decode_attn_static.
 hipError_t tetri_decode_static_memory(DecodeStatic *out);

@@ -9,7 +9,9 @@
 // one contiguous 16 * D * 2 bytes of a page, on the buffer side the tile is contiguous, so both sides
 // are touched in whole cache lines.  The page of a token is looked up once and reused for all slabs.
 // The data is used once: loads and stores are non-temporal.
-#include "attn_common.h"
+#include <type_traits>
+
+#include "cache_fp4.h"
 
 namespace {
 
@@ -177,7 +179,115 @@ __global__ __launch_bounds__(kThreads) void kv_export_fp8_kernel(const int32_t *
     while (slab < slab_end) st(ld());
 }
 
+// Export to 4-bit codes (cache_fp4.h): as kv_export_fp8_kernel, but a lane's 8 values become 4 bytes, and four lanes settle the exponent
+// they share.  Of a request's block the codes come first, [2 * Hkv][n][D / 2] bytes, then the exponents, [2 * Hkv][n][D / 32].
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv_export_fp4_kernel(const int32_t *cu, const int32_t *first, const int32_t *bt, const uint16_t *pool, int R,
+                                                                 int max_blocks, int Hkv, int slab_groups, uint32_t groups_magic, int slabs_per_wg,
+                                                                 char *buf)
+{
+    constexpr int LPR = D / 8, TILE = kThreads / LPR;
+    const int tid = threadIdx.x;
+    int tile, group;
+    tile_of(slab_groups, groups_magic, blockIdx.x, tile, group);
+    Tile x;
+    if (!find_tile<TILE>(cu, first, R, tile, tid & 63, x)) return;
+    const int j = x.j0 + tid / LPR;
+    if (j >= x.n) return;                                // (all lanes of a row leave together)
+    const int c = tid % LPR;
+    const int slabs = 2 * Hkv;
+    const int pos = x.first + j;
+    const int page = bt[(size_t)x.r * max_blocks + min(pos / kPage, max_blocks - 1)];
+    int slab = group * slabs_per_wg;
+    const int slab_end = min(slabs, slab + slabs_per_wg);
+    const size_t pool_step = (size_t)kPage * D;
+    const uint16_t *src = pool + ((size_t)page * slabs + slab) * pool_step + (size_t)(pos % kPage) * D + c * 8;
+    char *block = buf + (size_t)slabs * (D / 2 + D / 32) * x.c0;
+    char *codes = block + ((size_t)slab * x.n + j) * (D / 2) + c * 4;
+    char *exponents = block + (size_t)slabs * x.n * (D / 2) + ((size_t)slab * x.n + j) * (D / 32) + c / 4;
+    auto ld = [&]() {
+        const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src));
+        src += pool_step;
+        return v;
+    };
+    auto st = [&](const u32x4 &v) {
+        uint32_t e;
+        const uint32_t w = bf16_to_fp4(v, e);
+        // (a request's block begins at a multiple of 4 bytes)
+        __builtin_nontemporal_store(w, reinterpret_cast<uint32_t *>(codes));
+        if (c % 4 == 0) *reinterpret_cast<uint8_t *>(exponents) = (uint8_t)e;
+        codes += (size_t)x.n * (D / 2);
+        exponents += (size_t)x.n * (D / 32);
+        ++slab;
+    };
+#pragma unroll 1
+    while (slab + 4 <= slab_end) {
+        const u32x4 v0 = ld(), v1 = ld(), v2 = ld(), v3 = ld();
+        st(v0), st(v1), st(v2), st(v3);
+    }
+#pragma unroll 1
+    while (slab < slab_end) st(ld());
+}
+
+// Import of such a buffer into a pool of 4-bit codes, bytes as they are: a lane moves 16 bytes of a row's codes, the row's first lane its
+// exponents too.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv_import_fp4_kernel(const int32_t *cu, const int32_t *first, const int32_t *bt, char *pool, int R,
+                                                                 int max_blocks, int Hkv, int slab_groups, uint32_t groups_magic, int slabs_per_wg,
+                                                                 const char *buf)
+{
+    constexpr int LPR = D / 32, TILE = kThreads / LPR;
+    typedef u32x4 __attribute__((aligned(4))) u32x4_a4;  // (a request's block begins at a multiple of 4 bytes)
+    typedef std::conditional_t<D == 128, uint32_t, uint16_t> exponents_t;
+    const int tid = threadIdx.x;
+    int tile, group;
+    tile_of(slab_groups, groups_magic, blockIdx.x, tile, group);
+    Tile x;
+    if (!find_tile<TILE>(cu, first, R, tile, tid & 63, x)) return;
+    const int j = x.j0 + tid / LPR;
+    if (j >= x.n) return;
+    const int c = tid % LPR;
+    const int slabs = 2 * Hkv;
+    const int pos = x.first + j;
+    const int page = bt[(size_t)x.r * max_blocks + min(pos / kPage, max_blocks - 1)];
+    int slab = group * slabs_per_wg;
+    const int slab_end = min(slabs, slab + slabs_per_wg);
+    char *to = pool + ((size_t)page * slabs + slab) * kFp4Slab<D>;
+    const char *block = buf + (size_t)slabs * (D / 2 + D / 32) * x.c0;
+    const char *codes = block + ((size_t)slab * x.n + j) * (D / 2) + c * 16;
+    const char *exponents = block + (size_t)slabs * x.n * (D / 2) + ((size_t)slab * x.n + j) * (D / 32);
+    const int slot = pos % kPage;
+    for (; slab < slab_end; ++slab) {
+        const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a4 *>(codes));
+        exponents_t e = 0;
+        if (c == 0) e = *reinterpret_cast<const exponents_t *>(exponents);
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(to + slot * (D / 2) + c * 16));
+        if (c == 0) *reinterpret_cast<exponents_t *>(to + kFp4Codes<D> + slot * (D / 32)) = e;
+        codes += (size_t)x.n * (D / 2);
+        exponents += (size_t)x.n * (D / 32);
+        to += kFp4Slab<D>;
+    }
+}
+
 }  // namespace
+
+hipError_t tetri_launch_kv_export_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((tiles + kTilesAbreast - 1) / kTilesAbreast * kTilesAbreast * p.slab_groups)), block(kThreads);
+    auto kernel = h->cfg.head_dim == 128 ? kv_export_fp4_kernel<128> : kv_export_fp4_kernel<64>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.cu, p.first, p.bt, p.pool, p.R, p.max_blocks, p.Hkv, p.slab_groups, p.groups_magic,
+                       p.slabs_per_wg, reinterpret_cast<char *>(p.buf));
+    return hipGetLastError();
+}
+
+hipError_t tetri_launch_kv_import_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((tiles + kTilesAbreast - 1) / kTilesAbreast * kTilesAbreast * p.slab_groups)), block(kThreads);
+    auto kernel = h->cfg.head_dim == 128 ? kv_import_fp4_kernel<128> : kv_import_fp4_kernel<64>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, p.cu, p.first, p.bt, reinterpret_cast<char *>(p.pool), p.R, p.max_blocks, p.Hkv, p.slab_groups,
+                       p.groups_magic, p.slabs_per_wg, reinterpret_cast<const char *>(p.buf));
+    return hipGetLastError();
+}
 
 hipError_t tetri_launch_kv_export_fp8(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream)
 {

@@ -23,7 +23,7 @@ using namespace tetri_dev;
 typedef __attribute__((address_space(4))) const TilePlan const_plan;
 typedef __attribute__((address_space(4))) const u32x4 const_u32x4;
 
-template <int D, int KS, bool F8>
+template <int D, int KS, int BITS>
 __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_planned_kernel(AttnParams p, TilePlan)
 {
     constexpr int STAGE = Shape<KS>::STAGE, STAGE_U4 = STAGE * (D / 8), SLOTS = Shape<KS>::SLOTS, NT = Shape<KS>::WAVES * 64;
@@ -90,20 +90,20 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_planned_kernel(
 
     // ---- the first job's Q rows, by way of the second stage buffer (8 KB a wavefront; its first loads go out behind the job's
     // first barrier), and its first stage
-    Carry<D> cy;
+    Carry<D, BITS> cy;
     cy.par = J.it_begin & 1;                         // the first stage goes to buffer 0
     {
         char *q_tile = reinterpret_cast<char *>(smem + (wave < 4 ? 1 : 3) * STAGE_U4) + (wave & 3) * (32 * D * 2);
         request_q_rows<D>(p, J, J.grp * p.hpw + (slot & (p.hpw - 1)), slot >> p.hpw_shift, lane, lds_address(q_tile));
-        const WaveSrc ws = make_wave_src<D, KS, F8>(p, J.kh);
+        const WaveSrc ws = make_wave_src<D, KS, BITS>(p, J.kh);
         LaneOffsets<D> lo;
         init_lane_offsets<D>(lo, lane);
         const int page = load_stage_page<KS>(p.bt + J.src.bt_off, p.max_blocks, J.it_begin, wave);
         StageLoads sl;
-        const bool full = describe_stage_loads<D, KS, F8>(J.src, ws, lo, page, J.it_begin, wave, p.Hkv * D * 2, lds_address(smem), sl);
-        cy.have_codes = F8 && sl.codes;
-        if (F8 && sl.codes) {
-            fetch_stage_codes<D>(sl, full, cy.codes);
+        const bool full = describe_stage_loads<D, KS, BITS>(J.src, ws, lo, page, J.it_begin, wave, p.Hkv * D * 2, lds_address(smem), sl);
+        cy.have_codes = BITS < 16 && sl.codes;
+        if (BITS < 16 && sl.codes) {
+            if constexpr (BITS < 16) fetch_stage_codes<D>(sl, full, cy.codes);
             wait_vm<0>();
         } else {
             issue_stage_loads<D, KS>(sl, full);
@@ -126,7 +126,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_planned_kernel(
             }
             more = find_job(pj, after, N, after);
         }
-        tile_job<D, KS, F8, true>(p, first, &params, smem, Mstat, peek, old_stash, J, more, N, cy, ho);
+        tile_job<D, KS, BITS, true>(p, first, &params, smem, Mstat, peek, old_stash, J, more, N, cy, ho);
         if (!more) break;
         J = N;
     }
@@ -152,8 +152,8 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_planned_kernel(
 hipError_t tetri_launch_planned(const AttnParams &p, bool fp8_pool, hipStream_t stream)
 {
     static_assert(sizeof(AttnParams) + sizeof(TilePlan) + 16 <= 4096, "kernel arguments");
-    auto kernel = p.hpw * p.rb == 4 ? (fp8_pool ? attn_planned_kernel<128, 2, true> : attn_planned_kernel<128, 2, false>)
-                                    : (fp8_pool ? attn_planned_kernel<128, 3, true> : attn_planned_kernel<128, 3, false>);
+    auto kernel = p.hpw * p.rb == 4 ? (fp8_pool ? attn_planned_kernel<128, 2, 8> : attn_planned_kernel<128, 2, 16>)
+                                    : (fp8_pool ? attn_planned_kernel<128, 3, 8> : attn_planned_kernel<128, 3, 16>);
     // (the event rides on the kernel's own completion signal)
     if (p.plan->done) hipExtLaunchKernelGGL(kernel, dim3(p.attn_grid), dim3(512), 0, stream, nullptr, p.plan->done, 0, p, *p.plan);
     else hipLaunchKernelGGL(kernel, dim3(p.attn_grid), dim3(512), 0, stream, p, *p.plan);

@@ -106,6 +106,18 @@ class ChunkedPrefill:
     def attn_fp8(self, c, q, k_new, v_new, kv_pages_fp8, scale, k_scale, v_scale, append, out, stream=None):
         self._launch(c, q, k_new, v_new, kv_pages_fp8, scale, append, 1, k_scale, v_scale, out, stream)
 
+    def attn_fp4(self, c, q, k_new, v_new, kv_pages_fp4, scale, append, out, stream=None):
+        """Chunk c over a pool of 4-bit codes."""
+        cu, ctx, bt, S = self.meta[c]
+        self.handle.tetri_chunk_prefill_attn_fp4(q, k_new, v_new, kv_pages_fp4, bt, cu, ctx, S, scale, append, out, stream)
+
+    def qk_norm_rope(self, c, q, k, q_weight, k_weight, eps, rope, q_out, k_out, stream=None):
+        """q and k of chunk c's rows (two-dimensional, their rows may lie in a fused projection), normed where there are weights and
+        rotated by their positions, into q_out and k_out.  rope: a tetri.Rope."""
+        cu, ctx, _bt, S = self.meta[c]
+        self.handle.tetri_qk_norm_rope(q, q.stride(0), k, k.stride(0), q_weight, k_weight, eps, rope, None, cu, ctx, S, self.C, q_out, k_out,
+                                       stream)
+
     def weights_workspace(self, c, last_rows):
         """Bytes of device memory that weights() needs for chunk c."""
         return self.handle.tetri_chunk_prefill_weights_workspace(self.meta[c][3], self._longest_ctx(c), last_rows)

@@ -38,6 +38,34 @@ class Segment(ctypes.Structure):
     _fields_ = [("req", ctypes.c_int32), ("start", ctypes.c_int32), ("len", ctypes.c_int32)]
 
 
+TETRI_ROPE_PAIRS = 64
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("num_pairs", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("adjacent", ctypes.c_int32),
+                ("freq", ctypes.c_float * TETRI_ROPE_PAIRS), ("axis", ctypes.c_uint8 * TETRI_ROPE_PAIRS)]
+
+
+class Rope:
+    """A tetri_rope: radians per position of every pair and the axis whose position turns it (None: axis 0)."""
+
+    def __init__(self, freq, axis=None, num_axes=1, adjacent=False):
+        freq = np.ascontiguousarray(freq, dtype=np.float32).ravel()
+        n = len(freq)
+        axis = np.zeros(n, dtype=np.int64) if axis is None else np.asarray(axis, dtype=np.int64).ravel()
+        if n > TETRI_ROPE_PAIRS or len(axis) != n:
+            raise ValueError("%d frequencies (at most %d) and %d axes" % (n, TETRI_ROPE_PAIRS, len(axis)))
+        if n and (axis.min() < 0 or axis.max() >= num_axes):
+            raise ValueError("an axis is not in 0..%d" % (num_axes - 1))
+        self.struct = _RopeStruct(n, int(num_axes), int(bool(adjacent)))
+        self.struct.freq[:n] = freq.tolist()
+        self.struct.axis[:n] = axis.tolist()
+        self._p = ctypes.addressof(self.struct)
+
+    def data_ptr(self):
+        return self._p
+
+
 _lib = None
 
 
@@ -105,6 +133,16 @@ def lib():
         L.tetri_kv_select.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
         L.tetri_kv_compact.restype = i32
         L.tetri_kv_compact.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, vp]
+        L.tetri_kv_export_fp4.restype = i32
+        L.tetri_kv_export_fp4.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_int64, vp, vp]
+        L.tetri_kv_import_fp4.restype = i32
+        L.tetri_kv_import_fp4.argtypes = [vp, vp, vp, vp, vp, i32, ctypes.c_int64, vp, vp]
+        L.tetri_decode_attn_fp4.restype = i32
+        L.tetri_decode_attn_fp4.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, i32, vp, vp]
+        L.tetri_chunk_prefill_attn_fp4.restype = i32
+        L.tetri_chunk_prefill_attn_fp4.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp, vp]
+        L.tetri_qk_norm_rope.restype = i32
+        L.tetri_qk_norm_rope.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, f32, vp, vp, vp, vp, i32, i32, vp, vp, vp]
         L.tetri_validate_chunk.restype = i32
         L.tetri_validate_chunk.argtypes = [vp, vp, vp, vp, i32, vp]
         L.tetri_batch_create.restype = i32
@@ -395,6 +433,39 @@ class Tetri:
     def tetri_kv_compact(self, slots, block_table, ctx_lens, num_reqs, keep, recent, kv_pages, kv_weights, fp8, stream=None):
         rc = self._n.tetri_kv_compact(self._p, slots, block_table, ctx_lens, num_reqs, keep, recent, kv_pages, kv_weights, fp8,
                                       stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_kv_export_fp4(self, kv_pages, block_table, cu_tokens, first_tokens, num_reqs, total_tokens, buf, stream=None):
+        rc = self._n.tetri_kv_export_fp4(self._p, kv_pages, block_table, cu_tokens, first_tokens, num_reqs, total_tokens, buf, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_kv_import_fp4(self, buf, block_table, cu_tokens, first_tokens, num_reqs, total_tokens, kv_pages_fp4, stream=None):
+        rc = self._n.tetri_kv_import_fp4(self._p, buf, block_table, cu_tokens, first_tokens, num_reqs, total_tokens, kv_pages_fp4,
+                                         stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_decode_attn_fp4(self, q, k_new, v_new, kv_pages_fp4, block_table, ctx_lens, num_reqs, max_ctx_len, scale, append, out,
+                              stream=None):
+        rc = self._n.tetri_decode_attn_fp4(self._p, q, k_new, v_new, kv_pages_fp4, block_table, ctx_lens, num_reqs, max_ctx_len, scale,
+                                           append, out, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_chunk_prefill_attn_fp4(self, q, k_new, v_new, kv_pages_fp4, block_table, cu_chunk_q_lens, ctx_lens, num_segs, scale,
+                                     append, out, stream=None):
+        rc = self._n.tetri_chunk_prefill_attn_fp4(self._p, q, k_new, v_new, kv_pages_fp4, block_table, cu_chunk_q_lens, ctx_lens,
+                                                  num_segs, scale, append, out, stream)
+        if rc:
+            self._check(rc)
+
+    def tetri_qk_norm_rope(self, q, q_stride, k, k_stride, q_weight, k_weight, eps, rope, positions, cu_chunk_q_lens, ctx_lens,
+                           num_segs, num_rows, q_out, k_out, stream=None):
+        """rope: a Rope."""
+        rc = self._n.tetri_qk_norm_rope(self._p, q, q_stride, k, k_stride, q_weight, k_weight, eps, rope, positions, cu_chunk_q_lens,
+                                        ctx_lens, num_segs, num_rows, q_out, k_out, stream)
         if rc:
             self._check(rc)
 
