@@ -27,6 +27,9 @@ using namespace tetri_dev;
 
 constexpr int kMergeCols = 4;     // query heads whose partial O the merge area in LDS holds at a time
 constexpr int kWaves = 4;         // wavefronts of a workgroup
+// What a request costs a range of steps beside its steps, in steps: another page table, another Q, a merge.  A division that did not count it gave some ranges
+// five short requests and let all others wait for them (48 requests of 16 to 8192 tokens: 26.3 us, with it @@).
+constexpr int kRequestSteps = 8;
 
 // A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
 template <int D> __device__ __forceinline__ int part_floats(int g) { return g * D + ((2 * g + 3) & ~3); }
@@ -61,8 +64,20 @@ template <int D> struct Step {
     static constexpr int V = 2 * PAGE_BYTES, SCALES = 4 * PAGE_BYTES;
     static constexpr int BYTES = SCALES + (D == 128 ? 256 : 256);        // (an instruction of 64 lanes of 4 bytes)
     static constexpr int LOADS = D == 128 ? 5 : 3;                       // instructions
-    static constexpr int DEPTH = D == 128 ? 4 : 4;                       // steps a wavefront's ring holds
+    static constexpr int DEPTH = 2;                       // steps a wavefront's ring holds
 };
+
+// The sum of x over the lanes up to this one.
+__device__ __forceinline__ int prefix_sum(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // (from 1, 2, 4 and 8 lanes to the left in a row of 16)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // (a row's last lane to the next row, for rows 1 and 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // (lane 31 to rows 2 and 3)
+    return x;
+}
 
 // 64 lanes of 4 bytes, lane l's from base + off to LDS byte lds + 4 * l, past the caches as dma16_stream's.
 __device__ __forceinline__ void dma4_stream(const void *p, uint32_t lds)
@@ -81,7 +96,7 @@ constexpr int kDecodeLead = 56;   // bytes of the kernel's arguments in front of
 
 // NB: blocks of 16 query heads.  RANGES and the grid as decode_attn_kernel.
 template <int D, int NB, bool RANGES>
-__global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_t *ctx_lens, const int32_t *bt, const uint16_t *pages, int max_blocks, int Hkv,
+__global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kernel(const int32_t *ctx_lens, const int32_t *bt, const uint16_t *pages, int max_blocks, int Hkv,
                                                                     uint32_t hkv_magic, int parts, const uint16_t *q, int B, DecodeArgs)
 {
     typedef __attribute__((address_space(4))) const DecodeArgs const_decode_args;
@@ -90,7 +105,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
     __shared__ __attribute__((aligned(1024))) char smem[NW * DEPTH * T::BYTES];
     __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
     __shared__ float stat[NW][2][32];
-    __shared__ int arrived;
+    __shared__ int arrived[2];
     const const_decode_args *p = (const const_decode_args *)((__attribute__((address_space(4))) const char *)__builtin_amdgcn_kernarg_segment_ptr() + kDecodeLead);
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -100,7 +115,11 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
     // from a block-table index out of range
     auto ctx_of = [&](int b) -> int { return min(max(((const const_i32 *)(uintptr_t)ctx_lens)[b], 0), max_blocks * kPage); };
 
-    const int wg = magic_div(blockIdx.x, hkv_magic), kh = blockIdx.x - wg * Hkv;
+    // Two slabs are 17 cache lines, the one in the middle is both's: workgroups of neighbouring kv heads go to the same XCD (every 8th one),
+    // whose L2 then reads it once.
+    int item = blockIdx.x;
+    if ((item | 15) < (int)gridDim.x) item = (item & ~15) + 2 * (item & 7) + ((item >> 3) & 1);
+    const int wg = magic_div(item, hkv_magic), kh = item - wg * Hkv;
     auto clear_next = [&]() {
         const int n = p->n_counters;
         for (int i = blockIdx.x * NT + tid; i < n; i += gridDim.x * NT) store_global(p->counters_next + i, 0);
@@ -123,18 +142,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
         // lane l looks at requests l * R .. l * R + R - 1
         const int R = (B + 63) >> 6;
         const int32_t *ctx = ctx_lens;
-        auto steps_of = [&](int b) -> int { return max((min(max(ctx[b], 0), max_blocks * kPage) + 31) >> 5, 1); };
-        int mine = 0;
-        for (int i = 0; i < R; ++i) {
-            const int b = lane * R + i;
-            if (b < B) mine += steps_of(b);
-        }
-        int incl = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(incl, d, 64);
-            if (lane >= d) incl += y;
-        }
+        auto length_of = [&](int b) -> int { return min(max(ctx[min(b, B - 1)], 0), max_blocks * kPage); };
+        auto steps_of = [&](int L) -> int { return max((L + 31) >> 5, 1) + kRequestSteps; };
+        const int own = length_of(lane * R);             // (all there is to look at while there are no more than 64 requests)
+        int mine = lane * R < B ? steps_of(own) : 0;
+        for (int i = 1; i < R; ++i)
+            if (lane * R + i < B) mine += steps_of(length_of(lane * R + i));
+        const int incl = prefix_sum(mine);
         const int total = __builtin_amdgcn_readlane(incl, 63);
         const int ranges = min(p->ranges, (int)((uint32_t)(total + p->min_steps - 1) / (uint32_t)p->min_steps));
         if (wg >= ranges) {
@@ -147,19 +161,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
         left = div_q + (int)(wg < div_r);
         // the request of step `pos`: its lane, then inside the lane's block
         int base = incl - mine, found = -1, fl = 0, fbase = 0;
-        if (pos >= base && pos < incl)
-            for (int i = 0; i < R; ++i) {
-                const int b = min(lane * R + i, B - 1), n = steps_of(b);
-                if (found < 0 && pos < base + n) { found = b; fl = min(max(ctx[b], 0), max_blocks * kPage); fbase = base; }
-                base += n;
+        if (pos >= base && pos < incl) {
+            if (R == 1) {
+                found = lane; fl = own; fbase = base;
+            } else {
+                for (int i = 0; i < R; ++i) {
+                    const int L = length_of(lane * R + i), n = steps_of(L);
+                    if (found < 0 && pos < base + n) { found = min(lane * R + i, B - 1); fl = L; fbase = base; }
+                    base += n;
+                }
             }
+        }
         const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(found >= 0) | (1ull << 63));
         job.b = __builtin_amdgcn_readlane(found, src);
         if (job.b < 0) return;                           // (ctx_lens written to while the launch runs: no address is formed from it)
         job.L = __builtin_amdgcn_readlane(fl, src);
         job.begin = pos - __builtin_amdgcn_readlane(fbase, src);
         job.end = min(job.steps(), job.begin + left);
-        left -= job.end - job.begin;
+        left -= min(job.steps() + kRequestSteps - job.begin, left);
     }
     // the job after `j`, with `rest` steps of the range behind j: rest goes down by the new job's steps
     auto next_job = [&](Job &j, int &rest) {
@@ -167,8 +186,18 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
         j.L = ctx_of(min(j.b, B - 1));
         j.begin = 0;
         j.end = min(j.steps(), rest);
-        rest -= j.end;
+        rest -= min(j.steps() + kRequestSteps, rest);
     };
+    if constexpr (RANGES) {
+        if (job.begin >= job.end) {                      // (the range begins behind a request's steps)
+            if (left == 0) {
+                clear_next();
+                return;
+            }
+            pos += job.steps() + kRequestSteps - job.begin;
+            next_job(job, left);
+        }
+    }
 
     const uint32_t page_bytes = 2 * Hkv * kFp4Slab<D>, v_delta = Hkv * kFp4Slab<D>;
     const char *pool = reinterpret_cast<const char *>(pages) + (size_t)kh * kFp4Slab<D>;
@@ -193,22 +222,30 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
     if (s_is_v) s_off += v_delta;
 
     // ---- the wavefront's cursor: the step whose loads are issued next (step fs of job fj, frest steps of the range behind that job; fs < 0: there
-    // is none) and its pages
+    // is none).  The page ids of its next 32 steps are in the lanes of `ids`, the two of step id_first + NW * i in lanes 2i and 2i + 1: read by one
+    // vector load.  (Read step by step through the scalar cache, every wait for LDS waited for them too:)
     Job fj = job;
-    int fs = job.begin + wave, frest = left, pg0 = 0, pg1 = 0;
+    int fs = job.begin + wave, frest = left, id_at = 64;
+    int ids = 0;
     auto settle = [&]() {
         while (fs >= fj.end) {
             if (!RANGES || frest == 0) { fs = -1; return; }
             next_job(fj, frest);
             fs = wave;
+            id_at = 64;
         }
-        const int n = (fj.L + kPage - 1) / kPage;        // pages of the request
-        const const_i32 *row = (const const_i32 *)(uintptr_t)(bt + (size_t)fj.b * max_blocks);
-        pg0 = 2 * fs < n ? row[2 * fs] : 0;              // (a request without a token reads page 0 of the pool, and nothing of it counts)
-        pg1 = 2 * fs + 1 < n ? row[2 * fs + 1] : pg0;
+        if (id_at == 64) {
+            const int n = (fj.L + kPage - 1) / kPage;    // pages of the request; of what is not one, page 0 of the pool is read and does not count
+            const int e = 2 * (fs + NW * (lane >> 1)) + (lane & 1);
+            ids = 0;
+            if (e < n) ids = reinterpret_cast<__attribute__((address_space(1))) const int32_t *>((uintptr_t)(bt + (size_t)fj.b * max_blocks))[e];
+            id_at = 0;
+        }
     };
     auto issue = [&](int place) {
         const uint32_t lds = my_lds + place * T::BYTES;
+        const int pg0 = __builtin_amdgcn_readlane(ids, id_at), pg1 = __builtin_amdgcn_readlane(ids, id_at + 1);
+        id_at += 2;
         const char *a = pool + (size_t)pg0 * page_bytes, *b = pool + (size_t)pg1 * page_bytes;
         if constexpr (D == 128) {
             const uint32_t ko[1] = {k_off}, vo[1] = {v_off};
@@ -237,6 +274,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
                 u32x4 v = u32x4(qp[s]);
+                if (p->neg) v ^= 0x80008000u;            // (a negative scale is Q's sign)
                 if (col >= g) v = u32x4{0u, 0u, 0u, 0u};
                 qf[nb][s] = __builtin_bit_cast(bf16x8, v);
             }
@@ -248,7 +286,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
     int rb[DEPTH], rs[DEPTH], rL[DEPTH];                 // (a shift register: request, step and length of each)
     int place_in = 0, place_out = 0;
     settle();
-    const bool any = fs >= 0;
 #pragma unroll
     for (int i = 0; i < DEPTH; ++i) {
         rb[i] = 0; rs[i] = -1; rL[i] = 0;
@@ -262,17 +299,34 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
             settle();
         }
     }
-    (void)any;
 
-    const float c = p->neg ? -p->c : p->c;
+    const float c = p->c;
+    auto write_pair = [&](uint16_t *to, float x, float y, float l) {
+        const float inv = 1.0f / l;
+        bf16x2 r;
+        r[0] = (__bf16)(x * inv);
+        r[1] = (__bf16)(y * inv);
+        *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)to) = __builtin_bit_cast(uint32_t, r);
+    };
+    // What this workgroup has left of requests cut between workgroups, two at most (of its first job and of its last one): the request, its arrival
+    // counter, how many parts it has and where they are.  Settled when all jobs are done: a wait for the partial results' stores and the
+    // counter's answer are two trips to memory, and the loads of the jobs behind are in flight.
+    int cut_b[2], cut_counter[2], cut_pieces[2], cut_w0[2], cuts = 0;
+    auto place_of = [&](float *partial, int pfl, int w0, int i) -> float * {
+        return partial + ((size_t)(RANGES ? 2 * (w0 + i) + (int)(i == 0) : w0 + i) * Hkv + kh) * pfl;
+    };
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
 
     for (;;) {                                           // the jobs of the range
     f32x4 o[NB][DJ];
-    float m[NB], lsum[NB];                               // m: a reference exponent, not the exact maximum
+    f32x4 lsum[NB];                                      // the row sum, in every element: a product of ones and the weights as rounded
+    float m[NB];                                         // a reference exponent, not the exact maximum
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
         m[nb] = -1e30f;
-        lsum[nb] = 0.f;
+        lsum[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < DJ; ++j) o[nb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -286,67 +340,65 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
         case 3: wait_vm<2 * T::LOADS>(); break;
         default: wait_vm<3 * T::LOADS>(); break;
         }
-        static_assert(DEPTH == 4, "waits for up to three steps behind the current one");
+        static_assert(DEPTH <= 4, "waits for up to three steps behind the current one");
         const char *tile = my + place_out * T::BYTES;
-        // ---- scores
-        f32x4 sc[NB][2];
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-            const int row = 4 * (l16 & 3) + (l16 >> 2);
-            uint32_t kw[KS], e;
-            if constexpr (D == 128) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(tile + pg * T::PAGE_BYTES + row * 64 + ((grp ^ (row >> 2)) << 4));
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[s] = x[s];
-                e = *reinterpret_cast<const uint8_t *>(tile + T::SCALES + pg * (2 * T::SCALE_BYTES) + 4 * l16 + grp);
-            } else {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(tile + pg * T::PAGE_BYTES + row * 32 + grp * 8);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[s] = x[s];
-                e = *reinterpret_cast<const uint8_t *>(tile + T::SCALES + pg * (2 * T::SCALE_BYTES) + 2 * row + (grp >> 1));
-            }
-            const float scale = fp4_scale(e);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_to_bf16(kw[s], scale));
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nb][s], sc[nb][pg], 0, 0, 0);
-            }
-        }
-        // ---- V's codes and exponents: key 4i + grp of both pages
-        uint32_t vw[8];
+        // ---- the step's codes and exponents: K's rows, of V key 4i + grp of both pages
+        uint32_t kw[2][KS], ke[2], vw[8];
+        [[maybe_unused]] u32x4 ve[2];
         float vs[8];
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
-            const char *v = tile + T::V + pg * T::PAGE_BYTES, *es = tile + T::SCALES + (2 * pg + 1) * T::SCALE_BYTES;
+            const int row = 4 * (l16 & 3) + (l16 >> 2);
+            const char *k = tile + pg * T::PAGE_BYTES, *es = tile + T::SCALES + pg * (2 * T::SCALE_BYTES);
             if constexpr (D == 128) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(es + 16 * grp);
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(k + row * 64 + ((grp ^ (row >> 2)) << 4));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    vw[4 * pg + i] = *reinterpret_cast<const uint32_t *>(v + (4 * i + grp) * 64 + l16 * 4);
-                    vs[4 * pg + i] = fp4_scale((w[i] >> (8 * (l16 >> 2))) & 255u);
-                }
+                for (int s = 0; s < KS; ++s) kw[pg][s] = x[s];
+                ke[pg] = *reinterpret_cast<const uint8_t *>(es + 4 * l16 + grp);
+            } else {
+                const u32x2 x = *reinterpret_cast<const u32x2 *>(k + row * 32 + grp * 8);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kw[pg][s] = x[s];
+                ke[pg] = *reinterpret_cast<const uint8_t *>(es + 2 * row + (grp >> 1));
+            }
+        }
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+            const char *v = tile + T::V + pg * T::PAGE_BYTES, *es = tile + T::SCALES + (2 * pg + 1) * T::SCALE_BYTES;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (D == 128) vw[4 * pg + i] = *reinterpret_cast<const uint32_t *>(v + (4 * i + grp) * 64 + l16 * 4);
+                else vw[4 * pg + i] = *reinterpret_cast<const uint16_t *>(v + (4 * i + grp) * 32 + l16 * 2);
+            }
+            if constexpr (D == 128) {
+                ve[pg] = *reinterpret_cast<const u32x4 *>(es + 16 * grp);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    vw[4 * pg + i] = *reinterpret_cast<const uint16_t *>(v + (4 * i + grp) * 32 + l16 * 2);
-                    vs[4 * pg + i] = fp4_scale(*reinterpret_cast<const uint8_t *>(es + 2 * (4 * i + grp) + (l16 >> 3)));
-                }
+                for (int i = 0; i < 4; ++i) vs[4 * pg + i] = fp4_scale(*reinterpret_cast<const uint8_t *>(es + 2 * (4 * i + grp) + (l16 >> 3)));
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // everything is in registers: the place may be overwritten
         const bool far = fs >= 0;
         if (far) issue(place_in);
         if (++place_out == DEPTH) place_out = 0;
-        // ---- scores in units of log2, slots past the end masked
+        // (the byte of the lane's group turned to where a float has its exponent; what else is in the word the conversions do not look at)
+        if constexpr (D == 128) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+            for (int x = 0; x < 8; ++x) vs[x] = __builtin_bit_cast(float, __builtin_amdgcn_alignbit(ve[x / 4][x % 4], ve[x / 4][x % 4], 9 + 8 * (l16 >> 2)));
+        }
+        // ---- scores
+        f32x4 sc[NB][2];
 #pragma unroll
-            for (int pg = 0; pg < 2; ++pg)
+        for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sc[nb][pg][i] *= c;
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int pg = 0; pg < 2; ++pg) {
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_to_bf16(kw[pg][s], fp4_scale(ke[pg])));
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nb][s], sc[nb][pg], 0, 0, 0);
+            }
+        // ---- slots past the end are masked
         if (last) {
             const int n = cL - 32 * cs;                              // keys of the step
 #pragma unroll
@@ -363,13 +415,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             // m stays as it is unless a score exceeds it by 8 (weights are floating-point numbers: no precision is lost below)
-            float top = -INFINITY;
+            float top = sc[nb][0][0];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) top = fmaxf(top, sc[nb][x / 4][x % 4]);
-            if (__builtin_amdgcn_ballot_w64(top > m[nb] + 8.f) != 0) {
+            for (int x = 1; x < 8; ++x) top = fmaxf(top, sc[nb][x / 4][x % 4]);
+            if (__builtin_amdgcn_ballot_w64(top * c > m[nb] + 8.f) != 0) {
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(m[nb], top), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new);
+                const float m_new = fmaxf(m[nb], top * c), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new);
                 m[nb] = m_new;
                 lsum[nb] *= alpha;
 #pragma unroll
@@ -379,10 +431,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
             }
             // weights, rounded to bf16 for the PV product; the row sum is of the rounded ones
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                pf[nb][x] = (__bf16)__builtin_amdgcn_exp2f(sc[nb][x / 4][x % 4] - m[nb]);
-                lsum[nb] += (float)pf[nb][x];
-            }
+            for (int x = 0; x < 8; ++x) pf[nb][x] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[nb][x / 4][x % 4], c, -m[nb]));
+            lsum[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[nb], lsum[nb], 0, 0, 0);
         }
         // ---- O^T += V^T P^T
 #pragma unroll
@@ -440,7 +490,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
                 s *= c;
                 const float m_new = fmaxf(m[nb], s), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
                 m[nb] = m_new;
-                lsum[nb] = lsum[nb] * alpha + (grp == 0 ? w : 0.f);
+                lsum[nb] = lsum[nb] * alpha + w;
 #pragma unroll
                 for (int j = 0; j < DJ; ++j)
 #pragma unroll
@@ -471,10 +521,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
     const bool ends = job.end == job.steps(), whole = ends && job.begin == 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        float l = lsum[nb];
-        l += __shfl_xor(l, 16, 64);
-        l += __shfl_xor(l, 32, 64);
-        if (grp_e == 0) { stat[wave][0][16 * nb + l16_e] = m[nb]; stat[wave][1][16 * nb + l16_e] = l; }
+        if (grp_e == 0) { stat[wave][0][16 * nb + l16_e] = m[nb]; stat[wave][1][16 * nb + l16_e] = lsum[nb][0]; }
     }
     if (ends && e->pages_w != nullptr && job.L < max_blocks * kPage && wave == NW - 1 && (te & 63) < D / 4) {
         // fused append: the codes of the new token's K and V row of this kv head go to slot L % 16 of page block_table[b][L / 16], 8
@@ -510,17 +557,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
         counter = counter * Hkv + kh;
     }
     const int pfl = part_floats<D>(g);
-    float *partial = e->partial;
-    auto place = [&](int i) -> float * { return partial + ((size_t)(RANGES ? 2 * (w0 + i) + (int)(i == 0) : w0 + i) * Hkv + kh) * pfl; };
+    float *left_part = place_of(e->partial, pfl, w0, piece);
+    if (!whole) {
+        const bool second = cuts != 0;
+        if (!second) { cut_b[0] = job.b; cut_counter[0] = counter; cut_pieces[0] = pieces; cut_w0[0] = w0; }
+        else { cut_b[1] = job.b; cut_counter[1] = counter; cut_pieces[1] = pieces; cut_w0[1] = w0; }
+        ++cuts;
+    }
     const size_t head = (size_t)job.b * e->Hq + (size_t)kh * g;
-    uint16_t *out = e->out;
-    auto write_pair = [&](size_t at, float x, float y, float l) {
-        const float inv = 1.0f / l;
-        bf16x2 r;
-        r[0] = (__bf16)(x * inv);
-        r[1] = (__bf16)(y * inv);
-        *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)(out + at)) = __builtin_bit_cast(uint32_t, r);
-    };
+    uint16_t *out = e->out + head * D;
     for (int c0 = 0; c0 < g; c0 += kMergeCols) {
         if (c0 != 0) lds_barrier();                      // everybody is done with the columns before
 #pragma unroll
@@ -552,9 +597,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
                 l = __builtin_fmaf(stat[i][1][col], wgt, l);
             }
             if (whole) {
-                write_pair((head + col) * D + d, x, y, l);
+                write_pair(out + col * D + d, x, y, l);
             } else {
-                float *mine = place(piece);
+                float *mine = left_part;
                 store_coherent2(mine + col * D + d, x, y);
                 if (d == 0) {
                     store_coherent(mine + g * D + col, ms);
@@ -563,15 +608,29 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
             }
         }
     }
-    if (!whole) {
+    if (!RANGES || left == 0) break;
+    pos += job.steps() + kRequestSteps - job.begin;
+    next_job(job, left);
+    lds_barrier();                                       // everybody is done with stat and area
+    }
+
+    if (cuts != 0) {
+        const const_decode_args *e = p;
+        int te = tid;
+        asm volatile("" : "+v"(te), "+s"(e));
+        const int g = e->g, pfl = part_floats<D>(g);
+        float *partial = e->partial;
         coherent_stores_done();
         lds_barrier();
-        if (te == 0) arrived = atomic_add_global(e->counters + counter, 1);
+        if (te < cuts) arrived[te] = atomic_add_global(e->counters + (te == 0 ? cut_counter[0] : cut_counter[1]), 1);
         lds_barrier();
-        if (__builtin_amdgcn_readfirstlane(arrived) == pieces - 1) {
+        for (int k = 0; k < cuts; ++k) {
+            const int pieces = k == 0 ? cut_pieces[0] : cut_pieces[1], w0 = k == 0 ? cut_w0[0] : cut_w0[1];
+            if (__builtin_amdgcn_readfirstlane(arrived[k]) != pieces - 1) continue;
             // all the others have been here: the counter goes back to zero, the parts are merged in their order.  With few columns the
             // threads form groups that take every groups-th part, and the groups meet in LDS.
-            if (te == 0) store_global(e->counters + counter, 0);
+            if (te == 0) store_global(e->counters + (k == 0 ? cut_counter[0] : cut_counter[1]), 0);
+            uint16_t *rows = e->out + ((size_t)(k == 0 ? cut_b[0] : cut_b[1]) * e->Hq + (size_t)kh * g) * D;
             const int pairs = g * (D / 2), groups = max(1, NT / pairs);
             for (int v0 = 0; v0 < pairs; v0 += NT) {
                 const int grp_m = groups > 1 ? te / pairs : 0, v = groups > 1 ? te - grp_m * pairs : v0 + te;
@@ -584,7 +643,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
                         float2 xi[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float *src = place(min(i0 + i * groups, pieces - 1));
+                            const float *src = place_of(partial, pfl, w0, min(i0 + i * groups, pieces - 1));
                             mi[i] = load_coherent(src + g * D + col);
                             li[i] = load_coherent(src + g * D + g + col);
                             xi[i] = load_coherent2(src + 2 * v);
@@ -604,6 +663,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
                     // (a group without a part has m = -inf and weighs nothing; group 0 always has one)
                     float *meet = &area[0][0][0];
                     static_assert(NW * kMergeCols * D >= 4 * NT, "four floats per thread");
+                    lds_barrier();                       // everybody is done with what was merged before
                     if (on) *reinterpret_cast<f32x4 *>(meet + 4 * te) = f32x4{mm, l, x, y};
                     lds_barrier();
                     if (on && grp_m == 0)
@@ -617,14 +677,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void decode_fp4_kernel(const int32_
                             y = __builtin_fmaf(z[3], w_new, y * w_old);
                         }
                 }
-                if (on && grp_m == 0) write_pair(head * D + 2 * v, x, y, l);
+                if (on && grp_m == 0) write_pair(rows + 2 * v, x, y, l);
             }
         }
-    }
-    if (!RANGES || left == 0) break;
-    pos += job.end - job.begin;
-    next_job(job, left);
-    lds_barrier();                                       // everybody is done with stat, area and `arrived`
     }
     clear_next();
 }

@@ -381,15 +381,31 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     const int64_t places = room / part_bytes, cus = std::max(h->num_cus, 1);
     p.hkv_magic = p.Hkv <= 1 ? 0u : (uint32_t)((0x100000000ull + p.Hkv - 1) / p.Hkv);
     p.ranges = 0;
-    p.min_steps = h->decode_ranges > 0 ? 1 : 4;
-    const bool divisible = num_reqs <= kDecodeLookup && num_reqs * ((int64_t)cfg.max_blocks_per_seq * cfg.page_size / 32 + 1) <= 0x7fffffff;
+    p.min_steps = h->decode_ranges > 0 ? 1 : (fp4 ? 8 : 4);
+    // (9 steps more for each request: what the ranges over 4-bit codes count beside its steps)
+    const bool divisible = num_reqs <= kDecodeLookup && num_reqs * ((int64_t)cfg.max_blocks_per_seq * cfg.page_size / 32 + (fp4 ? 10 : 1)) <= 0x7fffffff;
     const int64_t most_bytes = pairs * steps * (fp4 ? 2 * 32 * (cfg.head_dim / 2 + cfg.head_dim / 32) : 32 * 2 * cfg.head_dim * (fp8 ? 1 : 2));
     int64_t parts = h->decode_parts;
     if (parts == 0) {
         parts = std::max<int64_t>(1, std::min(2 * cus / pairs, std::min<int64_t>((steps + 2) / 3, 32)));
         const int64_t most = std::min<int64_t>(places / 2, n_counters) / p.Hkv;
+        if (fp4) {
+            // Over 4-bit codes a step is short and what a workgroup costs besides counts for more.
+            //  - Parts: about as many as each then has steps, one workgroup per compute unit as long as that leaves none more than 24, otherwise two;
+            //    one part up to 12 steps.  (8 pairs of 251 steps: 16 parts 11.1 us, 8 12.6, 32 12.2; 32 pairs of 47: 6 8.3, 12 10.0, 1 13.3; 160
+            //    pairs of 10: 1 6.7, 2 8.9.)
+            //  - Ranges: long requests, fewer than four pairs to a compute unit, 128 MB if all contexts are as long as the longest; two to a compute unit,
+            //    for heads of 64 three.  (16 requests of 400 to 8000 tokens, 40 kv heads: 75.7 us, a workgroup per pair 95.9; 16 of 8000: 118 and 123; but 48 of
+            //    75 to 1500: 53.8 and 43.8.)
+            const int64_t root = (int64_t)std::lround(std::sqrt((double)steps));
+            parts = std::min(root, std::max<int64_t>(1, cus / pairs));
+            if (steps > 24 * parts) parts = std::max<int64_t>(1, std::min({root, 2 * cus / pairs, (int64_t)32}));
+            if (steps <= 12) parts = 1;
+            if (h->decode_ranges == 0 && pairs < 4 * cus && steps >= 128 && most_bytes >= 128000000 && divisible)
+                p.ranges = (int32_t)std::min((cfg.head_dim == 64 ? 3 : 2) * cus / p.Hkv, most);
+        }
         if (h->decode_ranges > 0 && divisible) p.ranges = (int32_t)std::min<int64_t>(h->decode_ranges, most);
-        else if (pairs < 2 * cus && most_bytes >= 200000000 && divisible) p.ranges = (int32_t)std::min(cus / p.Hkv, most);
+        else if (!fp4 && pairs < 2 * cus && most_bytes >= 200000000 && divisible) p.ranges = (int32_t)std::min(cus / p.Hkv, most);
     }
     if (p.ranges > 1) {
         p.parts = 0;
