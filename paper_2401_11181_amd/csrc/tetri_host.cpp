@@ -253,7 +253,7 @@ static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, vo
     // at a time closer together and leave no half-empty last round: 20000 tokens of 40x128 with 40 slabs each 203 us, with
     // 2 and 4 191.
     const int64_t slabs = 2 * (int64_t)p.Hkv;
-    p.slabs_per_wg = tiles * slabs <= 8 * (int64_t)std::max(h->num_cus, 1) ? 1 : (mode == 1 || mode == 3 ? 4 : 2);
+    p.slabs_per_wg = tiles * slabs <= 8 * (int64_t)std::max(h->num_cus, 1) ? 1 : (mode == 1 || mode == 3 || mode == 4 ? 4 : 2);
     if (h->transfer_slabs > 0) p.slabs_per_wg = h->transfer_slabs;
     p.slabs_per_wg = (int32_t)std::min<int64_t>(slabs, p.slabs_per_wg);
     p.slab_groups = (int32_t)((slabs + p.slabs_per_wg - 1) / p.slabs_per_wg);
@@ -1281,6 +1281,10 @@ tetri_status tetri_qk_norm_rope(tetri_ctx *h, const void *q, int64_t q_stride, c
     p.per_split = (int32_t)((insts + want - 1) / want);
     p.splits = (int32_t)((insts + p.per_split - 1) / p.per_split);
     p.splits_magic = p.splits <= 1 ? 0u : (uint32_t)((0x100000000ull + p.splits - 1) / p.splits);
+    // More than 64 MB of rows: read past the caches, where what is written then finds room, and what is read next.  (8192 rows of 32/8 heads 38.6 -> 32.7 us, with
+    // the chunk's attention behind it 116.9 -> 115.0; but 512 rows of 40 heads 7.3 and 7.9, with attention 31.1 and 32.0.  Writing past the caches is faster alone, 32.1
+    // and 6.4, and slower with the attention that reads it: 121.3.)
+    p.past_caches = (q_row + k_row) * 2 * num_rows > (64ll << 20);
     if ((uint64_t)num_rows * p.splits * p.splits + 4ull * p.splits >= 0x7fffffffull)
         return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many rows for one launch", fn);
     hipError_t e = tetri_launch_rope(cfg.head_dim, p, static_cast<hipStream_t>(stream));

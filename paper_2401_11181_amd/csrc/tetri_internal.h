@@ -369,6 +369,7 @@ struct RopeParams {
     int32_t splits;                   // wavefronts of a row, each of per_split instructions' heads
     uint32_t splits_magic;            // ceil(2^32 / splits), 0 for 1
     int32_t per_split;
+    int32_t past_caches;              // 1: the rows are read past the caches
     float freq[TETRI_ROPE_PAIRS];
     uint8_t axis[TETRI_ROPE_PAIRS];
 };

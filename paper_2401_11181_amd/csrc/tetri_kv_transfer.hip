@@ -257,16 +257,32 @@ __global__ __launch_bounds__(kThreads) void kv_import_fp4_kernel(const int32_t *
     const char *codes = block + ((size_t)slab * x.n + j) * (D / 2) + c * 16;
     const char *exponents = block + (size_t)slabs * x.n * (D / 2) + ((size_t)slab * x.n + j) * (D / 32);
     const int slot = pos % kPage;
-    for (; slab < slab_end; ++slab) {
-        const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a4 *>(codes));
-        exponents_t e = 0;
-        if (c == 0) e = *reinterpret_cast<const exponents_t *>(exponents);
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(to + slot * (D / 2) + c * 16));
-        if (c == 0) *reinterpret_cast<exponents_t *>(to + kFp4Codes<D> + slot * (D / 32)) = e;
-        codes += (size_t)x.n * (D / 2);
-        exponents += (size_t)x.n * (D / 32);
-        to += kFp4Slab<D>;
-    }
+    to += slot * (D / 2) + c * 16;
+    const size_t to_exponents = kFp4Codes<D> + slot * (D / 32) - (slot * (D / 2) + c * 16);
+    // (four slabs' loads in front of their stores)
+    auto move = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        u32x4 v[N];
+        exponents_t e[N] = {};
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a4 *>(codes + i * ((size_t)x.n * (D / 2))));
+            if (c == 0) e[i] = *reinterpret_cast<const exponents_t *>(exponents + i * ((size_t)x.n * (D / 32)));
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4 *>(to + i * kFp4Slab<D>));
+            if (c == 0) *reinterpret_cast<exponents_t *>(to + to_exponents + i * kFp4Slab<D>) = e[i];
+        }
+        codes += N * ((size_t)x.n * (D / 2));
+        exponents += N * ((size_t)x.n * (D / 32));
+        to += N * kFp4Slab<D>;
+        slab += N;
+    };
+#pragma unroll 1
+    while (slab + 4 <= slab_end) move(std::integral_constant<int, 4>());
+#pragma unroll 1
+    while (slab < slab_end) move(std::integral_constant<int, 1>());
 }
 
 }  // namespace
