@@ -3,23 +3,12 @@
 // same way; what a wavefront does with its steps is another thing, because codes are a quarter of the bytes: reading them is
 // 4.25 * D / 8 bytes per cached token and kv head, and at that rate the work per byte counts.
 //
-//   * A step is 32 keys, two pages, of one (request, kv head).  A slab of 1088 bytes (D = 128) comes straight into LDS: a page's codes by one
-//     instruction, the exponents of all four slabs of the step by one more.  A wavefront has a ring of kDepth steps of its own; no
-//     barrier stands between steps.
-//   * Codes become bf16 in registers, with their power of two (v_cvt_scalef32_pk_bf16_fp4, exact), and the products are 16x16x32 bf16 ones: sums are
-//     32-bit numbers.  (The products that take such codes and their exponents as they are, v_mfma_scale_f32_16x16x128_f8f6f4, need Q in 8-bit
-//     pieces, and they sum with fewer bits: of N(0, 1) scores of 128 products they lost 4e-6 of the root mean square, with one channel 50 times as large 3e-5 and
-//     up to 0.03 of a single score; this way 1e-8.)
-//   * S^T = K Q^T: the fragment of a lane is 8 neighbouring elements of a row, in any order over the lanes as long as Q's is the same: a lane takes
-//     D / 4 neighbouring codes of one key, which share an exponent.
-//   * O^T += V^T P^T needs several keys of one d in a lane, and codes of neighbouring d share a byte.  A lane reads D / 16 neighbouring codes of each of 8
-//     keys, converts pairs of them and puts the halves of two keys together (v_perm_b32): no transposition through LDS.  Row m of the
-//     product is then d = D / 16 * m + j, j its number.
-//   * Which key is which row of a page's product is free too: row 4a + b is key 4b + a, so that the rows which a V instruction reads are neighbours.
+// A step is 32 keys (fp4_steps.h).  A wavefront has a ring of steps of its own in LDS; no barrier stands between steps.
+//
 //   * Slots past the end of a request's cache may hold anything: their scores are masked, their exponents replaced (a code is
 //     finite, an exponent may stand for NaN).  Pages past the end are not looked up.
 //   * The new token is not quantised: its score is summed in 32 bits by the wavefront that has the request's last step.
-#include "cache_fp4.h"
+#include "fp4_steps.h"
 
 namespace {
 
@@ -27,27 +16,13 @@ using namespace tetri_dev;
 
 constexpr int kMergeCols = 4;     // query heads whose partial O the merge area in LDS holds at a time
 constexpr int kWaves = 4;         // wavefronts of a workgroup
+constexpr int kDepth = 2;         // steps a wavefront's ring holds: three workgroups fit a compute unit (with four steps, two: 64 requests of 2048 tokens 124.6 us, 119.6)
 // What a request costs a range of steps beside its steps, in steps: another page table, another Q, a merge.  A division that did not count it gave some ranges
 // five short requests and let all others wait for them (48 requests of 16 to 8192 tokens: 26.3 us, with it @@).
 constexpr int kRequestSteps = 8;
 
 // A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
 template <int D> __device__ __forceinline__ int part_floats(int g) { return g * D + ((2 * g + 3) & ~3); }
-
-__device__ __forceinline__ float load_coherent(const float *p)
-{
-    return __hip_atomic_load(reinterpret_cast<const __attribute__((address_space(1))) float *>((uintptr_t)p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 load_coherent2(const float *p)
-{
-    const uint64_t v = __hip_atomic_load(reinterpret_cast<const __attribute__((address_space(1))) uint64_t *>((uintptr_t)p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return make_float2(__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32)));
-}
-__device__ __forceinline__ void store_coherent2(float *p, float x, float y)
-{
-    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, x) | (uint64_t)__builtin_bit_cast(uint32_t, y) << 32;
-    __hip_atomic_store(reinterpret_cast<__attribute__((address_space(1))) uint64_t *>((uintptr_t)p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 
 // A stretch of steps of one request; wave-uniform.  A request without a cached token has one step, without keys.
 struct Job {
@@ -56,41 +31,6 @@ struct Job {
     int L;                      // cached tokens of the request
     __device__ __forceinline__ int steps() const { return max((L + 31) >> 5, 1); }
 };
-
-// A step in LDS: codes of K of both pages, of V of both, then the exponents of K and V of page 0 and K and V of page 1 (behind each other,
-// kScaleBytes of each; D = 128: row 4a + b of a slab's at place 4b + a).
-template <int D> struct Step {
-    static constexpr int ROW = D / 2, PAGE_BYTES = kPage * ROW, SCALE_BYTES = kPage * D / 32;
-    static constexpr int V = 2 * PAGE_BYTES, SCALES = 4 * PAGE_BYTES;
-    static constexpr int BYTES = SCALES + (D == 128 ? 256 : 256);        // (an instruction of 64 lanes of 4 bytes)
-    static constexpr int LOADS = D == 128 ? 5 : 3;                       // instructions
-    static constexpr int DEPTH = 2;                       // steps a wavefront's ring holds
-};
-
-// The sum of x over the lanes up to this one.
-__device__ __forceinline__ int prefix_sum(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // (from 1, 2, 4 and 8 lanes to the left in a row of 16)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // (a row's last lane to the next row, for rows 1 and 3)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // (lane 31 to rows 2 and 3)
-    return x;
-}
-
-// 64 lanes of 4 bytes, lane l's from base + off to LDS byte lds + 4 * l, past the caches as dma16_stream's.
-__device__ __forceinline__ void dma4_stream(const void *p, uint32_t lds)
-{
-    lds = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
-}
-// The same of 16 bytes, every lane with an address of its own.
-__device__ __forceinline__ void dma16_stream_lanes(const void *p, uint32_t lds)
-{
-    lds = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
-}
 
 constexpr int kDecodeLead = 56;   // bytes of the kernel's arguments in front of its structure (see tetri_decode.hip)
 
@@ -101,7 +41,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 {
     typedef __attribute__((address_space(4))) const DecodeArgs const_decode_args;
     typedef Step<D> T;
-    constexpr int NW = kWaves, NT = NW * 64, KS = D / 32, DJ = D / 16, DEPTH = T::DEPTH;
+    constexpr int NW = kWaves, NT = NW * 64, KS = D / 32, DJ = D / 16, DEPTH = kDepth;
     __shared__ __attribute__((aligned(1024))) char smem[NW * DEPTH * T::BYTES];
     __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
     __shared__ float stat[NW][2][32];
@@ -204,22 +144,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
     char *my = smem + wave * (DEPTH * T::BYTES);
     const uint32_t my_lds = lds_address(my);
 
-    // ---- where a lane's part of a step comes from.  K, D = 128: place (row, c) of LDS has chunk c ^ row / 4 of the row (16 bytes), so that the
-    // 16 lanes that read the same chunk of all rows meet no bank twice.
-    const uint32_t k_off = D == 128 ? (lane >> 2) * 64 + (((lane & 3) ^ (lane >> 4)) << 4) : (lane & 31) * 16;
-    const uint32_t v_off = D == 128 ? lane * 16 : (lane & 31) * 16;
-    uint32_t s_off;                                      // ... of the slab's exponents
-    bool s_second, s_is_v;                               // ... of which page, and of V
-    if constexpr (D == 128) {
-        s_off = kFp4Codes<D> + (4 * (l16 & 3) + (l16 >> 2)) * 4;
-        s_is_v = (grp & 1) != 0;
-        s_second = grp >= 2;
-    } else {                                             // (lanes past 32 read once more what the others do)
-        s_off = kFp4Codes<D> + (lane & 7) * 4;
-        s_is_v = (lane & 8) != 0;
-        s_second = (lane & 16) != 0;
-    }
-    if (s_is_v) s_off += v_delta;
+    const StepSource<D> source(lane, v_delta);
 
     // ---- the wavefront's cursor: the step whose loads are issued next (step fs of job fj, frest steps of the range behind that job; fs < 0: there
     // is none).  The page ids of its next 32 steps are in the lanes of `ids`, the two of step id_first + NW * i in lanes 2i and 2i + 1: read by one
@@ -243,26 +168,12 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
         }
     };
     auto issue = [&](int place) {
-        const uint32_t lds = my_lds + place * T::BYTES;
         const int pg0 = __builtin_amdgcn_readlane(ids, id_at), pg1 = __builtin_amdgcn_readlane(ids, id_at + 1);
         id_at += 2;
-        const char *a = pool + (size_t)pg0 * page_bytes, *b = pool + (size_t)pg1 * page_bytes;
-        if constexpr (D == 128) {
-            const uint32_t ko[1] = {k_off}, vo[1] = {v_off};
-            dma16_stream<1>(a, ko, lds);
-            dma16_stream<1>(b, ko, lds + T::PAGE_BYTES);
-            dma4_stream((s_second ? b : a) + s_off, lds + T::SCALES);
-            dma16_stream<1>(a + v_delta, vo, lds + T::V);
-            dma16_stream<1>(b + v_delta, vo, lds + T::V + T::PAGE_BYTES);
-        } else {
-            const char *mine = lane < 32 ? a : b;
-            dma16_stream_lanes(mine + k_off, lds);
-            dma4_stream((s_second ? b : a) + s_off, lds + T::SCALES);
-            dma16_stream_lanes(mine + v_delta + v_off, lds + T::V);
-        }
+        issue_step<D>(source, pool + (size_t)pg0 * page_bytes, pool + (size_t)pg1 * page_bytes, v_delta, lane, my_lds + place * T::BYTES);
     };
     // Q fragments (B operand of S^T): column l16 is query head kh * g + l16 of the block, zero past g; element 8 s .. of a lane's D / 4 ones
-    bf16x8 qf[NB][KS];
+    Columns<D, NB> x;
     auto load_q = [&](int b) {
         int ln = lane;
         asm volatile("" : "+v"(ln));
@@ -276,7 +187,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
                 u32x4 v = u32x4(qp[s]);
                 if (p->neg) v ^= 0x80008000u;            // (a negative scale is Q's sign)
                 if (col >= g) v = u32x4{0u, 0u, 0u, 0u};
-                qf[nb][s] = __builtin_bit_cast(bf16x8, v);
+                x.qf[nb][s] = __builtin_bit_cast(bf16x8, v);
             }
         }
     };
@@ -315,21 +226,8 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
     auto place_of = [&](float *partial, int pfl, int w0, int i) -> float * {
         return partial + ((size_t)(RANGES ? 2 * (w0 + i) + (int)(i == 0) : w0 + i) * Hkv + kh) * pfl;
     };
-    bf16x8 ones;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
-
     for (;;) {                                           // the jobs of the range
-    f32x4 o[NB][DJ];
-    f32x4 lsum[NB];                                      // the row sum, in every element: a product of ones and the weights as rounded
-    float m[NB];                                         // a reference exponent, not the exact maximum
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-        m[nb] = -1e30f;
-        lsum[nb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < DJ; ++j) o[nb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    x.clear();
     while (rs[0] >= 0 && (!RANGES || rb[0] == job.b)) {
         const int cb = rb[0], cs = rs[0], cL = rL[0];
         const bool last = cs + 1 == max((cL + 31) >> 5, 1);          // the request's last step
@@ -342,62 +240,15 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
         }
         static_assert(DEPTH <= 4, "waits for up to three steps behind the current one");
         const char *tile = my + place_out * T::BYTES;
-        // ---- the step's codes and exponents: K's rows, of V key 4i + grp of both pages
-        uint32_t kw[2][KS], ke[2], vw[8];
-        [[maybe_unused]] u32x4 ve[2];
-        float vs[8];
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-            const int row = 4 * (l16 & 3) + (l16 >> 2);
-            const char *k = tile + pg * T::PAGE_BYTES, *es = tile + T::SCALES + pg * (2 * T::SCALE_BYTES);
-            if constexpr (D == 128) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(k + row * 64 + ((grp ^ (row >> 2)) << 4));
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[pg][s] = x[s];
-                ke[pg] = *reinterpret_cast<const uint8_t *>(es + 4 * l16 + grp);
-            } else {
-                const u32x2 x = *reinterpret_cast<const u32x2 *>(k + row * 32 + grp * 8);
-#pragma unroll
-                for (int s = 0; s < KS; ++s) kw[pg][s] = x[s];
-                ke[pg] = *reinterpret_cast<const uint8_t *>(es + 2 * row + (grp >> 1));
-            }
-        }
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-            const char *v = tile + T::V + pg * T::PAGE_BYTES, *es = tile + T::SCALES + (2 * pg + 1) * T::SCALE_BYTES;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (D == 128) vw[4 * pg + i] = *reinterpret_cast<const uint32_t *>(v + (4 * i + grp) * 64 + l16 * 4);
-                else vw[4 * pg + i] = *reinterpret_cast<const uint16_t *>(v + (4 * i + grp) * 32 + l16 * 2);
-            }
-            if constexpr (D == 128) {
-                ve[pg] = *reinterpret_cast<const u32x4 *>(es + 16 * grp);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) vs[4 * pg + i] = fp4_scale(*reinterpret_cast<const uint8_t *>(es + 2 * (4 * i + grp) + (l16 >> 3)));
-            }
-        }
+        StepCodes<D> codes;
+        codes.read(tile, grp, l16);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // everything is in registers: the place may be overwritten
         const bool far = fs >= 0;
         if (far) issue(place_in);
         if (++place_out == DEPTH) place_out = 0;
-        // (the byte of the lane's group turned to where a float has its exponent; what else is in the word the conversions do not look at)
-        if constexpr (D == 128) {
-#pragma unroll
-            for (int x = 0; x < 8; ++x) vs[x] = __builtin_bit_cast(float, __builtin_amdgcn_alignbit(ve[x / 4][x % 4], ve[x / 4][x % 4], 9 + 8 * (l16 >> 2)));
-        }
-        // ---- scores
+        codes.powers(l16);
         f32x4 sc[NB][2];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int pg = 0; pg < 2; ++pg) {
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, fp4_to_bf16(kw[pg][s], fp4_scale(ke[pg])));
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nb][s], sc[nb][pg], 0, 0, 0);
-            }
+        x.scores(codes, sc);
         // ---- slots past the end are masked
         if (last) {
             const int n = cL - 32 * cs;                              // keys of the step
@@ -406,59 +257,14 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (16 * pg + 4 * i + grp >= n) {
-                        vs[4 * pg + i] = 0.f;
+                        codes.vs[4 * pg + i] = 0.f;
 #pragma unroll
                         for (int nb = 0; nb < NB; ++nb) sc[nb][pg][i] = -INFINITY;
                     }
         }
         bf16x8 pf[NB];
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            // m stays as it is unless a score exceeds it by 8 (weights are floating-point numbers: no precision is lost below)
-            float top = sc[nb][0][0];
-#pragma unroll
-            for (int x = 1; x < 8; ++x) top = fmaxf(top, sc[nb][x / 4][x % 4]);
-            if (__builtin_amdgcn_ballot_w64(top * c > m[nb] + 8.f) != 0) {
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(m[nb], top * c), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new);
-                m[nb] = m_new;
-                lsum[nb] *= alpha;
-#pragma unroll
-                for (int j = 0; j < DJ; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nb][j][i] *= alpha;
-            }
-            // weights, rounded to bf16 for the PV product; the row sum is of the rounded ones
-#pragma unroll
-            for (int x = 0; x < 8; ++x) pf[nb][x] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(sc[nb][x / 4][x % 4], c, -m[nb]));
-            lsum[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[nb], lsum[nb], 0, 0, 0);
-        }
-        // ---- O^T += V^T P^T
-#pragma unroll
-        for (int t = 0; t < DJ / 2; ++t) {
-            uint32_t x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                bf16x2 y;
-                if (t == 0) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 0);
-                else if (t == 1) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 1);
-                else if (t == 2) y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 2);
-                else y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vw[k], vs[k], 3);
-                x[k] = __builtin_bit_cast(uint32_t, y);
-            }
-            u32x4 even, odd;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                even[k] = __builtin_amdgcn_perm(x[2 * k + 1], x[2 * k], 0x05040100u);
-                odd[k] = __builtin_amdgcn_perm(x[2 * k + 1], x[2 * k], 0x07060302u);
-            }
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                o[nb][2 * t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pf[nb], o[nb][2 * t], 0, 0, 0);
-                o[nb][2 * t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pf[nb], o[nb][2 * t + 1], 0, 0, 0);
-            }
-        }
+        x.weigh(sc, c, pf);
+        x.add(codes, pf);
         if (last) {
             // the new token: a lane has D / 4 products of its score, and the rows of O that it holds
             const size_t at = ((size_t)cb * Hkv + kh) * D;
@@ -484,17 +290,17 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(value(kn[k], j), value(__builtin_bit_cast(u32x4, qf[nb][k]), j), s);
+                    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(value(kn[k], j), value(__builtin_bit_cast(u32x4, x.qf[nb][k]), j), s);
                 s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
                 s *= c;
-                const float m_new = fmaxf(m[nb], s), alpha = __builtin_amdgcn_exp2f(m[nb] - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
-                m[nb] = m_new;
-                lsum[nb] = lsum[nb] * alpha + w;
+                const float m_new = fmaxf(x.m[nb], s), alpha = __builtin_amdgcn_exp2f(x.m[nb] - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
+                x.m[nb] = m_new;
+                x.lsum[nb] = x.lsum[nb] * alpha + w;
 #pragma unroll
                 for (int j = 0; j < DJ; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nb][j][i] = __builtin_fmaf(w, value(vn[i], j), o[nb][j][i] * alpha);
+                    for (int i = 0; i < 4; ++i) x.o[nb][j][i] = __builtin_fmaf(w, value(vn[i], j), x.o[nb][j][i] * alpha);
             }
         }
         // on to the next step (its Q rows, if it is another request's, are requested here)
@@ -521,7 +327,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
     const bool ends = job.end == job.steps(), whole = ends && job.begin == 0;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-        if (grp_e == 0) { stat[wave][0][16 * nb + l16_e] = m[nb]; stat[wave][1][16 * nb + l16_e] = lsum[nb][0]; }
+        if (grp_e == 0) { stat[wave][0][16 * nb + l16_e] = x.m[nb]; stat[wave][1][16 * nb + l16_e] = x.lsum[nb][0]; }
     }
     if (ends && e->pages_w != nullptr && job.L < max_blocks * kPage && wave == NW - 1 && (te & 63) < D / 4) {
         // fused append: the codes of the new token's K and V row of this kv head go to slot L % 16 of page block_table[b][L / 16], 8
@@ -571,14 +377,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int col = 16 * nb + l16_e;
-            if (col >= c0 && col < min(g, c0 + kMergeCols)) {
-                float *mine = area[wave][col - c0];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < DJ; j += 4)
-                        *reinterpret_cast<f32x4 *>(mine + DJ * (4 * grp_e + i) + j) = f32x4{o[nb][j][i], o[nb][j + 1][i], o[nb][j + 2][i], o[nb][j + 3][i]};
-            }
+            if (col >= c0 && col < min(g, c0 + kMergeCols)) x.put(nb, area[wave][col - c0], grp_e);
         }
         lds_barrier();
         // two neighbouring values of one head per thread
@@ -587,20 +386,20 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
             float ms = stat[0][0][col];
 #pragma unroll
             for (int i = 1; i < NW; ++i) ms = fmaxf(ms, stat[i][0][col]);
-            float x = 0.f, y = 0.f, l = 0.f;
+            float v0 = 0.f, v1 = 0.f, l = 0.f;
 #pragma unroll
             for (int i = 0; i < NW; ++i) {
                 const float wgt = __builtin_amdgcn_exp2f(stat[i][0][col] - ms);
                 const float2 z = *reinterpret_cast<const float2 *>(&area[i][cc][d]);
-                x = __builtin_fmaf(z.x, wgt, x);
-                y = __builtin_fmaf(z.y, wgt, y);
+                v0 = __builtin_fmaf(z.x, wgt, v0);
+                v1 = __builtin_fmaf(z.y, wgt, v1);
                 l = __builtin_fmaf(stat[i][1][col], wgt, l);
             }
             if (whole) {
-                write_pair(out + col * D + d, x, y, l);
+                write_pair(out + col * D + d, v0, v1, l);
             } else {
                 float *mine = left_part;
-                store_coherent2(mine + col * D + d, x, y);
+                store_coherent2(mine + col * D + d, v0, v1);
                 if (d == 0) {
                     store_coherent(mine + g * D + col, ms);
                     store_coherent(mine + g * D + g + col, l);

@@ -980,6 +980,34 @@ static int32_t new_row_stores(const tetri_ctx *h, int32_t num_segs, bool fp8, in
     return rows * row * (h->cfg.num_q_heads + h->cfg.num_kv_heads) <= 28 << 20 ? kRowsThrough : kRowsCached;
 }
 
+// The shape of a launch of the kernel of small tiles over 4-bit codes; false where its numbers do not fit.
+static bool plan_small_tiles(const tetri_ctx *h, int32_t num_segs, bool append, PrefillFp4Params &p)
+{
+    const tetri_config &cfg = h->cfg;
+    p.S = num_segs; p.C = cfg.chunk_size; p.Hq = cfg.num_q_heads; p.Hkv = cfg.num_kv_heads; p.g = p.Hq / p.Hkv; p.max_blocks = cfg.max_blocks_per_seq;
+    p.g_magic = p.g <= 1 ? 0u : (uint32_t)((0x100000000ull + p.g - 1) / p.g);
+    p.hkv_magic = p.Hkv <= 1 ? 0u : (uint32_t)((0x100000000ull + p.Hkv - 1) / p.Hkv);
+    // the rows go to their slots by a workgroup for every 64 KB
+    p.append_blocks = append ? (int32_t)std::max<int64_t>(8, std::min<int64_t>(64, (int64_t)p.C * p.Hkv * cfg.head_dim * 4 >> 16)) : 0;
+    const int64_t places = 2 * (int64_t)std::max(h->num_cus, 1) - p.append_blocks, part_bytes = (int64_t)kPrefillFp4Cols * (cfg.head_dim + 2) * 4;
+    int64_t ranges = std::max<int64_t>(1, places / p.Hkv);
+    ranges = std::min<int64_t>(ranges, (int64_t)(2 * h->scratch_units * h->unit_bytes) / (2 * part_bytes * p.Hkv));
+    ranges = std::min<int64_t>(ranges, h->n_counters / p.Hkv);
+    p.ranges = (int32_t)ranges;
+    p.min_steps = 8;
+    // (positions of the sequence, columns times query heads and workgroups times kv heads are 32-bit numbers in the kernel)
+    const int64_t columns = (int64_t)p.C * p.g, tiles = columns / kPrefillFp4Cols + num_segs;
+    return ranges >= 1 && tiles * ((int64_t)p.max_blocks / 2 + p.C / 32 + 8) <= 0x7fffffff && (columns + kPrefillFp4Cols) * p.g < 0xffffffffll &&
+           ranges * p.Hkv * p.Hkv < 0xffffffffll;
+}
+// Whether a chunk goes there.
+static bool small_tiles_preferred(const tetri_ctx *h, int32_t num_segs)
+{
+    (void)h;
+    (void)num_segs;
+    return true;
+}
+
 static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new,
                                 const void *kv_pages, void *kv_pages_w, const int32_t *block_table, const int32_t *cu,
                                 const int32_t *ctx_lens, int32_t num_segs, float scale, void *out, void *stream,
@@ -1051,6 +1079,26 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
         return TETRI_OK;
     }
     if (carry && (st = send_metadata(h, fn, *carry, hs)) != TETRI_OK) return st;
+    // ---- 4-bit codes: the kernel of small tiles
+    PrefillFp4Params fp;
+    if (fp4 && (h->attn_variant == 3 || (h->attn_variant == 0 && !h->division_set && small_tiles_preferred(h, num_segs))) &&
+        plan_small_tiles(h, num_segs, kv_pages_w != nullptr, fp)) {
+        fp.q = p.q; fp.k_new = p.k_new; fp.v_new = p.v_new; fp.pages = p.pages; fp.pages_w = p.pages_w; fp.out = p.out;
+        fp.bt = p.bt; fp.cu = p.cu; fp.ctx = p.ctx;
+        fp.c = p.c; fp.neg = p.neg;
+        const bool capturing = stream_captures(hs);
+        if ((st = claim_scratch(h, fn, hs, capturing)) != TETRI_OK) return st;
+        fp.scratch = reinterpret_cast<float *>(h->scratch);
+        fp.n_counters = h->n_counters;
+        const CounterSets cs = counter_sets(h->counters, h->n_counters, h->counter_turn);
+        fp.counters = cs.use;
+        fp.counters_next = cs.clear;
+        hipError_t e = tetri_launch_prefill_fp4(h->cfg.head_dim, fp, hs);
+        if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
+        ++h->counter_turn;
+        if (!capturing) scratch_claimed(h, hs);
+        return TETRI_OK;
+    }
     auto log2i = [](int v) { int s = 0; while ((1 << s) < v) ++s; return s; };
     // ---- the other chunks whose segments the host knows: the shared-tile kernel on a division made here
     if (host_cu && !stream_captures(hs)) {

@@ -355,6 +355,26 @@ struct CompactParams {
     int32_t B, Hkv, max_blocks, keep, recent;
 };
 
+// Prefill over a pool of 4-bit codes in tiles of 32 columns (tetri_prefill_fp4.hip).
+constexpr int32_t kPrefillFp4Cols = 32;
+struct PrefillFp4Params {
+    const uint16_t *q, *k_new, *v_new, *pages;
+    uint16_t *pages_w;            // pool for the fused append
+    uint16_t *out;
+    const int32_t *bt, *cu, *ctx;
+    int32_t S, C, Hq, Hkv, g, max_blocks;
+    uint32_t g_magic, hkv_magic;  // ceil(2^32 / d), 0 for 1
+    float c;                      // |scale| * log2(e)
+    int32_t neg;                  // 1 if scale < 0
+    int32_t ranges;               // workgroups of a kv head
+    int32_t min_steps;            // ... each of at least this many steps
+    int32_t append_blocks;        // workgroups that cache the chunk's rows (0: nobody does)
+    float *scratch;               // partial results, two to a workgroup
+    int32_t *counters;            // arrival counters, one to a workgroup, zero before and after the launch
+    int32_t *counters_next;       // the set of a later launch: zeroed by this one
+    int32_t n_counters;           // size of a set
+};
+
 // Norm and rotation of queries and keys (tetri_rope.hip).
 struct RopeParams {
     const uint16_t *q, *k;            // rows of q_stride and k_stride elements
@@ -383,6 +403,7 @@ hipError_t tetri_launch_kv_transfer(const tetri_ctx *h, const TransferParams &p,
 hipError_t tetri_launch_kv_export_fp8(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);
 // The same over a pool of 4-bit codes (tetri_decode_fp4.hip).
 hipError_t tetri_launch_decode_fp4(const tetri_ctx *h, const DecodeParams &p, hipStream_t stream);
+hipError_t tetri_launch_prefill_fp4(int head_dim, const PrefillFp4Params &p, hipStream_t stream);
 hipError_t tetri_launch_rope(int head_dim, const RopeParams &p, hipStream_t stream);
 hipError_t tetri_launch_kv_export_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);
 hipError_t tetri_launch_kv_import_fp4(const tetri_ctx *h, const TransferParams &p, int32_t tiles, hipStream_t stream);

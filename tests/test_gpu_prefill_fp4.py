@@ -15,7 +15,7 @@ from test_gpu_parity import CASES, VARIANTS
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(params=VARIANTS, ids=["auto", "wave4", "wave8", "tails", "tails-wave4", "whole", "tails-half", "stream5", "stream5-wave4", "stream2", "stream200"])
+@pytest.fixture(params=VARIANTS + [3], ids=["auto", "wave4", "wave8", "tails", "tails-wave4", "whole", "tails-half", "stream5", "stream5-wave4", "stream2", "stream200", "small-tiles"])
 def variant(request):
     return request.param
 
