@@ -92,7 +92,8 @@ typedef struct {
  * Partial results are kept there, in two parts.
  *   - One part is shared by the chunk-prefill launches that divide themselves (all without host metadata, and those with it that
  *     "attn_variant" below names) where they are small enough to be divided over the compute units by stages rather than by row
- *     tiles, by those for little work that split the keys of their row blocks, and by the decode calls where they split
+ *     tiles, by those for little work that split the keys of their row blocks, by those over 4-bit codes that go to the kernel of
+ *     smaller tiles ("attn_variant" below), and by the decode calls where they split
  *     requests: such launches on one handle must not overlap in time; use one handle per stream that runs concurrently.  A
  *     chunk-prefill call returns TETRI_ERR_INVALID_ARG when the handle's previous such chunk-prefill launch went to another
  *     stream and that stream still has work pending (synchronise the two streams, or use a handle each); decode calls neither
@@ -627,6 +628,8 @@ TETRI_API tetri_status tetri_validate_chunk(tetri_ctx *ctx, const int32_t *block
  *                       workgroups of that launch; 3 = the kernel for chunks with little work wherever its tables hold
  *                       the chunk; 4 / 5 = a division of the launch made on the host, with row tiles of 8 / 4 (head, 32-row
  *                       block) slots, wherever the call knows the chunk's segments and the tables hold it (head_dim 128);
+ *                       over 4-bit codes 0 = the library chooses between that launch and a kernel of smaller tiles (always the launch once one of
+ *                       the split_* options or stream_wgs has been set), 3 = that kernel, 1 / 2 = the launch;
  *   "split_keys"        1 (default) = a launch that divides itself, with fewer than five row tiles per four compute units, divides
  *                       the key ranges of its tiles among more workgroups than it has tiles (a launch on the host's division of any
  *                       size: see attn_variant 4 / 5).  If the tiles and one helper
@@ -635,19 +638,20 @@ TETRI_API tetri_status tetri_validate_chunk(tetri_ctx *ctx, const int32_t *block
  *                       more on average, and at most 64 segments) the stages (64 or 128 keys each) of all row
  *                       tiles of a head group are laid end to end and every workgroup of the group gets an equal
  *                       range of them.  Tiles shared by several workgroups are finished from partial results in
- *                       the handle's scratch memory (see tetri_create).  0 = no tile is shared;
+ *                       the handle's scratch memory (see tetri_create).  Over 4-bit codes stages are laid end to end for any segments, unless tiles and
+ *                       helpers of long ones fill four fifths of the compute units.  0 = no tile is shared;
  *   "split_min_stages"  tails: key ranges of fewer stages than this are not divided (default 8; at least 2);
  *   "split_bias_stages" tails: stages a tile keeps before the rest is shared (default 6; not negative);
  *   "split_share_q8"    tails: share of that rest the helper takes, in 1/256 (default 85; 1..128);
  *   "stream_wgs"        workgroups per head group when the stages are laid end to end (default 0: as many as
  *                       the device has compute units for); a value of 1..255 also forces that division for
  *                       launches of any size with at most 64 segments;
- *   "decode_parts"      workgroups that share the keys of one (request, kv head) in tetri_decode_attn
+ *   "decode_parts"      workgroups that share the keys of one (request, kv head) in tetri_decode_attn and its kin
  *                       (default 0: chosen from num_reqs and max_ctx_len);
  *   "decode_ranges"     the steps of a decode batch in that many equal ranges per kv head, each a workgroup's,
  *                       whatever the context lengths (default 0: chosen like decode_parts; decode_parts, where
  *                       set, comes first);
- *   "transfer_slabs"    (K / V, head) slabs one workgroup of tetri_kv_export / tetri_kv_import moves
+ *   "transfer_slabs"    (K / V, head) slabs one workgroup of tetri_kv_export / tetri_kv_import (_fp8, _fp4) moves
  *                       (default 0: chosen from the size of the transfer).
  * Unknown keys or values give TETRI_ERR_INVALID_ARG.  Every setting computes the same
  * function to the same tolerance.

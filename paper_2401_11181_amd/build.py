@@ -9,9 +9,11 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtetri.so")
 NATIVE = os.path.join(HERE, "_native.so")
-SOURCES = ["tetri_host.cpp", "tetri_evict_host.cpp", "tetri_plan.cpp", "tetri_append.hip", "tetri_kv_transfer.hip", "tetri_decode.hip", "tetri_decode_fp4.hip", "tetri_prefill_fp4.hip", "tetri_rope.hip", "tetri_attn.hip", "tetri_planned.hip", "tetri_short.hip",
-           "tetri_weights.hip", "tetri_evict.hip"]
-HEADERS = [os.path.join(CSRC, "tetri_internal.h"), os.path.join(CSRC, "tetri_plan.h"), os.path.join(CSRC, "attn_common.h"), os.path.join(CSRC, "cache_fp4.h"), os.path.join(CSRC, "fp4_steps.h"), os.path.join(CSRC, "attn_tile.h"), os.path.join(ROOT, "include", "tetri.h")]
+SOURCES = ["tetri_host.cpp", "tetri_evict_host.cpp", "tetri_fp4_host.cpp", "tetri_rope_host.cpp", "tetri_plan.cpp", "tetri_append.hip",
+           "tetri_kv_transfer.hip", "tetri_decode.hip", "tetri_decode_fp4.hip", "tetri_prefill_fp4.hip", "tetri_rope.hip", "tetri_attn.hip",
+           "tetri_planned.hip", "tetri_short.hip", "tetri_weights.hip", "tetri_evict.hip"]
+HEADERS = [os.path.join(CSRC, name) for name in ("tetri_internal.h", "tetri_plan.h", "attn_common.h", "cache_fp4.h", "fp4_steps.h", "attn_tile.h")] + \
+          [os.path.join(ROOT, "include", "tetri.h")]
 
 # packed-fp32 instructions are switched off for all device code; a kernel's leading scalar arguments (up to 14 words in front of
 # its first structure) are in registers when a wavefront starts, instead of a first memory read away

@@ -55,17 +55,30 @@ __device__ __forceinline__ int prefix_sum(int x)
     return x;
 }
 
-// 64 lanes of 4 bytes, lane l's from base + off to LDS byte lds + 4 * l, past the caches as dma16_stream's.
-__device__ __forceinline__ void dma4_stream(const void *p, uint32_t lds)
+// 64 lanes of 4 bytes, lane l's from p to LDS byte lds + 4 * l, and of 16 bytes; ONCE: read once, past the caches as dma16_stream's.
+template <bool ONCE> __device__ __forceinline__ void dma4_lanes(const void *p, uint32_t lds)
 {
     lds = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+    if constexpr (ONCE) asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dword %0, off" ::"v"(p), "s"(lds) : "memory", "m0");
 }
-// The same of 16 bytes, every lane with an address of its own.
-__device__ __forceinline__ void dma16_stream_lanes(const void *p, uint32_t lds)
+template <bool ONCE> __device__ __forceinline__ void dma16_lanes(const void *p, uint32_t lds)
 {
     lds = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+    if constexpr (ONCE) asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(p), "s"(lds) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(p), "s"(lds) : "memory", "m0");
+}
+// 64 lanes of 16 bytes from base + off.
+template <bool ONCE> __device__ __forceinline__ void dma16_base(const void *base, uint32_t off, uint32_t lds)
+{
+    if constexpr (ONCE) {
+        const uint32_t v[1] = {off};
+        dma16_stream<1>(base, v, lds);
+    } else {
+        base = uniform_ptr(base);
+        lds = __builtin_amdgcn_readfirstlane(lds);
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+    }
 }
 
 // Where a lane's part of a step comes from.
@@ -89,23 +102,22 @@ template <int D> struct StepSource {
         }
     }
 };
-// The loads of a step; a, b: the slabs of K of its pages (the same kv head), lds: its place.
-template <int D>
+// The loads of a step; a, b: the slabs of K of its pages (the same kv head), lds: its place.  ONCE: nobody else reads them.
+template <int D, bool ONCE>
 __device__ __forceinline__ void issue_step(const StepSource<D> &x, const char *a, const char *b, uint32_t v_delta, int lane, uint32_t lds)
 {
     typedef Step<D> T;
     if constexpr (D == 128) {
-        const uint32_t ko[1] = {x.k_off}, vo[1] = {x.v_off};
-        dma16_stream<1>(a, ko, lds);
-        dma16_stream<1>(b, ko, lds + T::PAGE_BYTES);
-        dma4_stream((x.s_second ? b : a) + x.s_off, lds + T::SCALES);
-        dma16_stream<1>(a + v_delta, vo, lds + T::V);
-        dma16_stream<1>(b + v_delta, vo, lds + T::V + T::PAGE_BYTES);
+        dma16_base<ONCE>(a, x.k_off, lds);
+        dma16_base<ONCE>(b, x.k_off, lds + T::PAGE_BYTES);
+        dma4_lanes<ONCE>((x.s_second ? b : a) + x.s_off, lds + T::SCALES);
+        dma16_base<ONCE>(a + v_delta, x.v_off, lds + T::V);
+        dma16_base<ONCE>(b + v_delta, x.v_off, lds + T::V + T::PAGE_BYTES);
     } else {
         const char *mine = lane < 32 ? a : b;
-        dma16_stream_lanes(mine + x.k_off, lds);
-        dma4_stream((x.s_second ? b : a) + x.s_off, lds + T::SCALES);
-        dma16_stream_lanes(mine + v_delta + x.v_off, lds + T::V);
+        dma16_lanes<ONCE>(mine + x.k_off, lds);
+        dma4_lanes<ONCE>((x.s_second ? b : a) + x.s_off, lds + T::SCALES);
+        dma16_lanes<ONCE>(mine + v_delta + x.v_off, lds + T::V);
     }
 }
 
@@ -115,7 +127,7 @@ template <int D> struct StepCodes {
     u32x4 ve[2];                         // D = 128: exponents of all groups, a word for each key
     float vs[8];
     // reads them; they have arrived when LDS reads have been waited for
-    __device__ __forceinline__ void read(const char *tile, int grp, int l16)
+    __device__ __forceinline__ void read_k(const char *tile, int grp, int l16)
     {
         typedef Step<D> T;
 #pragma unroll
@@ -134,6 +146,10 @@ template <int D> struct StepCodes {
                 ke[pg] = *reinterpret_cast<const uint8_t *>(es + 2 * row + (grp >> 1));
             }
         }
+    }
+    __device__ __forceinline__ void read_v(const char *tile, int grp, int l16)
+    {
+        typedef Step<D> T;
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
             const char *v = tile + T::V + pg * T::PAGE_BYTES, *es = tile + T::SCALES + (2 * pg + 1) * T::SCALE_BYTES;
@@ -158,6 +174,13 @@ template <int D> struct StepCodes {
             for (int x = 0; x < 8; ++x) vs[x] = __builtin_bit_cast(float, __builtin_amdgcn_alignbit(ve[x / 4][x % 4], ve[x / 4][x % 4], 9 + 8 * (l16 >> 2)));
         }
     }
+    __device__ __forceinline__ void negate_k()
+    {
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) kw[pg][s] ^= 0x88888888u;
+    }
     __device__ __forceinline__ bf16x8 k(int pg, int s) const { return __builtin_bit_cast(bf16x8, fp4_to_bf16(kw[pg][s], fp4_scale(ke[pg]))); }
     // elements 2t and 2t + 1 of V of key x
     template <int TT> __device__ __forceinline__ uint32_t v(int x) const
@@ -169,7 +192,6 @@ template <int D> struct StepCodes {
 // NB blocks of 16 columns (queries) and what attention over some keys has made of them.
 template <int D, int NB> struct Columns {
     static constexpr int KS = D / 32, DJ = D / 16;
-    bf16x8 qf[NB][KS];                   // B operand of S^T: elements 8 s .. of a lane's D / 4
     f32x4 o[NB][DJ];                     // element i: row 4 * grp + i of product j
     f32x4 lsum[NB];                      // the row sum, in every element: a product of ones and the weights as rounded
     float m[NB];                         // a reference exponent, not the exact maximum
@@ -184,19 +206,21 @@ template <int D, int NB> struct Columns {
             for (int j = 0; j < DJ; ++j) o[nb][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
-    // scores of a step's keys; K: something with k(page, s)
-    template <class K> __device__ __forceinline__ void scores(const K &codes, f32x4 (&sc)[NB][2]) const
+    // scores of a step's keys; K: something with k(page, s); q(nb, s): B operand, elements 8 s .. of a lane's D / 4 of column block nb
+    template <class K, class Q> static __device__ __forceinline__ void scores(const K &codes, const Q &q, f32x4 (&sc)[NB][2])
     {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) sc[nb][0] = sc[nb][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+        for (int s = 0; s < KS; ++s) {
+            const bf16x8 k0 = codes.k(0, s), k1 = codes.k(1, s);
 #pragma unroll
-            for (int pg = 0; pg < 2; ++pg) {
-                const bf16x8 kf = codes.k(pg, s);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) sc[nb][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[nb][s], sc[nb][pg], 0, 0, 0);
+            for (int nb = 0; nb < NB; ++nb) {
+                const bf16x8 qf = q(nb, s);
+                sc[nb][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf, sc[nb][0], 0, 0, 0);
+                sc[nb][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf, sc[nb][1], 0, 0, 0);
             }
+        }
     }
     // their weights: rounded to bf16 for the PV product, the row sum is of the rounded ones.  c > 0
     __device__ __forceinline__ void weigh(const f32x4 (&sc)[NB][2], float c, bf16x8 (&pf)[NB])

@@ -127,6 +127,11 @@ __device__ __forceinline__ void zero_padding_rows(const AttnParams &p, int grp, 
     }
 }
 
+// Stream mode over 4-bit codes: with fewer stages than this to a tile on average, a tile is not cut.  (A segment of 512 rows without context, 32 heads over 8:
+// 19.4 us, cut 23.7; 128 rows in 6 segments without much, 40 heads: 14.6 and 19.3; but behind 500 cached tokens 8 heads over 2, 128 rows, 23.0 and
+// 18.5.)
+constexpr int kWholeStages = 4;
+
 template <int D, int KS, int BITS>
 __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(AttnParams p)
 {
@@ -189,6 +194,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     // stages shared by Gp workgroups; the tile the next job is in: tile j of nt in its segment,
     // starting at position tile_lin
     int pos = 0, b1 = 0, W = 1, Gp = 1, j = 0, nt = 1, tile_lin = 0, tile_index = 0;
+    bool whole_tiles = false;                        // ... or, over 4-bit codes, one tile to a workgroup
     // stream mode, one segment whose block-table row fits two registers per lane: the whole row is fetched together
     // with the segment lengths, so that the pages of the workgroup's first stage, wherever its range starts, do not
     // cost a second round trip to memory
@@ -338,12 +344,20 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         // the padding rows, shared by the G workgroups of the group
         zero_padding_rows<D>(p, grp, widx, G, tid, NT);
         Gp = min(G, W);
+        // Over 4-bit codes the host, which does not know the segments, also sends chunks of short ones here: where every tile finds a workgroup and has
+        // few stages, cutting them gains less than putting the pieces together costs.
+        if constexpr (BITS == 4) {
+            const int T = __builtin_amdgcn_readlane(t_incl, 63);
+            whole_tiles = T <= G && W < kWholeStages * T;
+            if (whole_tiles) Gp = T;
+        }
         if (widx >= Gp) return;
         // (the divisions run on the vector unit: their results are marked as the wave-uniform values they are)
         // and the host has checked that no product below reaches 2^31)
         pos = __builtin_amdgcn_readfirstlane((int)((uint32_t)(widx * W) / (uint32_t)Gp));
         b1 = __builtin_amdgcn_readfirstlane((int)((uint32_t)((widx + 1) * W) / (uint32_t)Gp));
-        const unsigned long long owner = __builtin_amdgcn_ballot_w64(pos >= w_incl - wk && pos < w_incl);
+        unsigned long long owner = __builtin_amdgcn_ballot_w64(pos >= w_incl - wk && pos < w_incl);
+        if (BITS == 4 && whole_tiles) owner = __builtin_amdgcn_ballot_w64(widx >= t_incl - ntl && widx < t_incl);
         if (owner == 0) return;                      // cannot happen for well-formed metadata
         const int o = __builtin_ctzll(owner);
         seg.s = o;
@@ -366,7 +380,9 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
             j = j0 + cnt - 1;
             if (cnt < 64) break;
         }
+        if (BITS == 4 && whole_tiles) j = widx - __builtin_amdgcn_readlane(t_incl - ntl, o);
         tile_lin = seg_lin + j * cs + new_stages_before<STAGE>(j, bm_shift);
+        if (BITS == 4 && whole_tiles) { pos = tile_lin; b1 = W; }
         tile_index = __builtin_amdgcn_readlane(t_incl - ntl, o) + j;
     }
 
@@ -383,6 +399,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         X.npieces = wl - X.wf + 1;
         X.piece = widx - X.wf;
         pos = tile_lin + X.it_end;
+        if (BITS == 4 && whole_tiles) { X.wf = widx; X.npieces = 1; X.piece = 0; b1 = pos; }
         if (pos == tile_end) {
             tile_lin = tile_end;
             ++tile_index;
@@ -503,19 +520,20 @@ hipError_t launch(const AttnParams &p, hipStream_t stream)
 
 }  // namespace
 
-hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, int pool_bits, hipStream_t stream)
+hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, bool fp8_pool, hipStream_t stream)
 {
-    if (p.plan != nullptr) return pool_bits == 4 ? hipErrorInvalidValue : tetri_launch_planned(p, pool_bits == 8, stream);
+    if (p.plan != nullptr) return tetri_launch_planned(p, fp8_pool, stream);
     const bool wide = h->cfg.head_dim == 128;
-    switch (pool_bits) {
-    case 4:
-        if (wide) return key_parts == 2 ? launch<128, 2, 4>(p, stream) : launch<128, 1, 4>(p, stream);
-        return key_parts == 2 ? launch<64, 2, 4>(p, stream) : launch<64, 1, 4>(p, stream);
-    case 8:
+    if (fp8_pool) {
         if (wide) return key_parts == 2 ? launch<128, 2, 8>(p, stream) : launch<128, 1, 8>(p, stream);
         return key_parts == 2 ? launch<64, 2, 8>(p, stream) : launch<64, 1, 8>(p, stream);
-    default:
-        if (wide) return key_parts == 2 ? launch<128, 2, 16>(p, stream) : launch<128, 1, 16>(p, stream);
-        return key_parts == 2 ? launch<64, 2, 16>(p, stream) : launch<64, 1, 16>(p, stream);
     }
+    if (wide) return key_parts == 2 ? launch<128, 2, 16>(p, stream) : launch<128, 1, 16>(p, stream);
+    return key_parts == 2 ? launch<64, 2, 16>(p, stream) : launch<64, 1, 16>(p, stream);
+}
+
+hipError_t tetri_launch_attn_fp4(const tetri_ctx *h, const AttnParams &p, int key_parts, hipStream_t stream)
+{
+    if (h->cfg.head_dim == 128) return key_parts == 2 ? launch<128, 2, 4>(p, stream) : launch<128, 1, 4>(p, stream);
+    return key_parts == 2 ? launch<64, 2, 4>(p, stream) : launch<64, 1, 4>(p, stream);
 }

@@ -18,7 +18,7 @@ constexpr int kMergeCols = 4;     // query heads whose partial O the merge area 
 constexpr int kWaves = 4;         // wavefronts of a workgroup
 constexpr int kDepth = 2;         // steps a wavefront's ring holds: three workgroups fit a compute unit (with four steps, two: 64 requests of 2048 tokens 124.6 us, 119.6)
 // What a request costs a range of steps beside its steps, in steps: another page table, another Q, a merge.  A division that did not count it gave some ranges
-// five short requests and let all others wait for them (48 requests of 16 to 8192 tokens: 26.3 us, with it @@).
+// five short requests and let all others wait for them (48 requests of 16 to 8192 tokens, 32 heads over 8: 33.0 us, with it 20.3).
 constexpr int kRequestSteps = 8;
 
 // A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 
     // ---- the wavefront's cursor: the step whose loads are issued next (step fs of job fj, frest steps of the range behind that job; fs < 0: there
     // is none).  The page ids of its next 32 steps are in the lanes of `ids`, the two of step id_first + NW * i in lanes 2i and 2i + 1: read by one
-    // vector load.  (Read step by step through the scalar cache, every wait for LDS waited for them too:)
+    // vector load.  (Read step by step through the scalar cache they share a counter with LDS, and every wait for codes waited for them too.)
     Job fj = job;
     int fs = job.begin + wave, frest = left, id_at = 64;
     int ids = 0;
@@ -164,15 +164,17 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
             const int e = 2 * (fs + NW * (lane >> 1)) + (lane & 1);
             ids = 0;
             if (e < n) ids = reinterpret_cast<__attribute__((address_space(1))) const int32_t *>((uintptr_t)(bt + (size_t)fj.b * max_blocks))[e];
+            wait_vm<0>();                                // (here, once in 32 steps: the compiler's own wait stands at every step, where it drains the loads in flight)
             id_at = 0;
         }
     };
     auto issue = [&](int place) {
         const int pg0 = __builtin_amdgcn_readlane(ids, id_at), pg1 = __builtin_amdgcn_readlane(ids, id_at + 1);
         id_at += 2;
-        issue_step<D>(source, pool + (size_t)pg0 * page_bytes, pool + (size_t)pg1 * page_bytes, v_delta, lane, my_lds + place * T::BYTES);
+        issue_step<D, true>(source, pool + (size_t)pg0 * page_bytes, pool + (size_t)pg1 * page_bytes, v_delta, lane, my_lds + place * T::BYTES);
     };
     // Q fragments (B operand of S^T): column l16 is query head kh * g + l16 of the block, zero past g; element 8 s .. of a lane's D / 4 ones
+    bf16x8 qf[NB][KS];
     Columns<D, NB> x;
     auto load_q = [&](int b) {
         int ln = lane;
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
                 u32x4 v = u32x4(qp[s]);
                 if (p->neg) v ^= 0x80008000u;            // (a negative scale is Q's sign)
                 if (col >= g) v = u32x4{0u, 0u, 0u, 0u};
-                x.qf[nb][s] = __builtin_bit_cast(bf16x8, v);
+                qf[nb][s] = __builtin_bit_cast(bf16x8, v);
             }
         }
     };
@@ -241,14 +243,15 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
         static_assert(DEPTH <= 4, "waits for up to three steps behind the current one");
         const char *tile = my + place_out * T::BYTES;
         StepCodes<D> codes;
-        codes.read(tile, grp, l16);
+        codes.read_k(tile, grp, l16);
+        codes.read_v(tile, grp, l16);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // everything is in registers: the place may be overwritten
         const bool far = fs >= 0;
         if (far) issue(place_in);
         if (++place_out == DEPTH) place_out = 0;
         codes.powers(l16);
         f32x4 sc[NB][2];
-        x.scores(codes, sc);
+        x.scores(codes, [&](int nb, int s) { return qf[nb][s]; }, sc);
         // ---- slots past the end are masked
         if (last) {
             const int n = cL - 32 * cs;                              // keys of the step
@@ -290,7 +293,7 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(value(kn[k], j), value(__builtin_bit_cast(u32x4, x.qf[nb][k]), j), s);
+                    for (int j = 0; j < 8; ++j) s = __builtin_fmaf(value(kn[k], j), value(__builtin_bit_cast(u32x4, qf[nb][k]), j), s);
                 s += __shfl_xor(s, 16, 64);
                 s += __shfl_xor(s, 32, 64);
                 s *= c;

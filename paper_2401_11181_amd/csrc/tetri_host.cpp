@@ -220,7 +220,7 @@ tetri_status tetri_kv_append(tetri_ctx *h, const void *k_new, const void *v_new,
 static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, void *buf, const int32_t *block_table,
                                 const int32_t *cu_tokens, const int32_t *first_tokens, int32_t num_reqs,
                                 int64_t total_tokens, bool to_pool, void *stream, int mode = 0, float k_scale = 1.f,
-                                float v_scale = 1.f)
+                                float v_scale = 1.f, const Fp4Launchers *fp4 = nullptr)
 {
     if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
     if (!kv_pages || !aligned16(kv_pages)) return fail(h, TETRI_ERR_INVALID_ARG, "%s: kv_pages is null or not 16-byte aligned", fn);
@@ -262,8 +262,8 @@ static tetri_status kv_transfer(const char *fn, tetri_ctx *h, void *kv_pages, vo
         return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many tokens for one launch", fn);
     p.k_inv = 1.0f / k_scale; p.v_inv = 1.0f / v_scale;
     hipError_t e = mode == 1 ? tetri_launch_kv_export_fp8(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
-                 : mode == 3 ? tetri_launch_kv_export_fp4(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
-                 : mode == 4 ? tetri_launch_kv_import_fp4(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
+                 : mode == 3 ? fp4->export_codes(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
+                 : mode == 4 ? fp4->import_codes(h, p, (int32_t)tiles, static_cast<hipStream_t>(stream))
                              : tetri_launch_kv_transfer(h, p, row_units, (int32_t)tiles, to_pool, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return TETRI_OK;
@@ -285,21 +285,6 @@ tetri_status tetri_kv_import_fp8(tetri_ctx *h, const void *buf, const int32_t *b
                        first_tokens, num_reqs, total_tokens, true, stream, 2);
 }
 
-tetri_status tetri_kv_export_fp4(tetri_ctx *h, const void *kv_pages, const int32_t *block_table, const int32_t *cu_tokens,
-                                 const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *buf, void *stream)
-{
-    return kv_transfer("tetri_kv_export_fp4", h, const_cast<void *>(kv_pages), buf, block_table, cu_tokens, first_tokens,
-                       num_reqs, total_tokens, false, stream, 3);
-}
-
-tetri_status tetri_kv_import_fp4(tetri_ctx *h, const void *buf, const int32_t *block_table, const int32_t *cu_tokens,
-                                 const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *kv_pages_fp4,
-                                 void *stream)
-{
-    return kv_transfer("tetri_kv_import_fp4", h, kv_pages_fp4, const_cast<void *>(buf), block_table, cu_tokens,
-                       first_tokens, num_reqs, total_tokens, true, stream, 4);
-}
-
 tetri_status tetri_kv_export(tetri_ctx *h, const void *kv_pages, const int32_t *block_table, const int32_t *cu_tokens,
                              const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, void *buf, void *stream)
 {
@@ -318,7 +303,8 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
                                   const void *kv_pages, void *kv_pages_w, const int32_t *block_table,
                                   const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
                                   void *stream, bool fp8 = false, float k_scale = 1.f, float v_scale = 1.f,
-                                  bool static_scratch = false, const DecodeWeights *weights = nullptr, bool fp4 = false)
+                                  bool static_scratch = false, const DecodeWeights *weights = nullptr,
+                                  const Fp4Launchers *fp4 = nullptr)
 {
     if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
     const void *ptrs[] = {q, k_new, v_new, kv_pages, out};
@@ -429,7 +415,7 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     p.weights_w = weights ? weights->weights_w : nullptr;
     p.score_stride = weights ? weights->score_stride : 0;
     p.max_ctx = weights ? weights->max_ctx : 0;
-    hipError_t e = fp4 ? tetri_launch_decode_fp4(h, p, static_cast<hipStream_t>(stream)) : tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
+    hipError_t e = fp4 ? fp4->decode(h, p, static_cast<hipStream_t>(stream)) : tetri_launch_decode(h, p, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares && !static_scratch) ++h->counter_turn;
     return TETRI_OK;
@@ -459,15 +445,6 @@ tetri_status tetri_decode_attn_fp8(tetri_ctx *h, const void *q, const void *k_ne
     if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_decode_attn_fp8: append must be 0 or 1");
     return decode_common("tetri_decode_attn_fp8", h, q, k_new, v_new, kv_pages_fp8, append ? kv_pages_fp8 : nullptr,
                          block_table, ctx_lens, num_reqs, max_ctx_len, scale, out, stream, true, k_scale, v_scale);
-}
-
-tetri_status tetri_decode_attn_fp4(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages_fp4, const int32_t *block_table,
-                                   const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, int32_t append, void *out,
-                                   void *stream)
-{
-    if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_decode_attn_fp4: append must be 0 or 1");
-    return decode_common("tetri_decode_attn_fp4", h, q, k_new, v_new, kv_pages_fp4, append ? kv_pages_fp4 : nullptr, block_table, ctx_lens,
-                         num_reqs, max_ctx_len, scale, out, stream, false, 1.f, 1.f, false, nullptr, true);
 }
 
 tetri_status tetri_decode_attn_append(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages,
@@ -989,7 +966,7 @@ static bool plan_small_tiles(const tetri_ctx *h, int32_t num_segs, bool append, 
     p.hkv_magic = p.Hkv <= 1 ? 0u : (uint32_t)((0x100000000ull + p.Hkv - 1) / p.Hkv);
     // the rows go to their slots by a workgroup for every 64 KB
     p.append_blocks = append ? (int32_t)std::max<int64_t>(8, std::min<int64_t>(64, (int64_t)p.C * p.Hkv * cfg.head_dim * 4 >> 16)) : 0;
-    const int64_t places = 2 * (int64_t)std::max(h->num_cus, 1) - p.append_blocks, part_bytes = (int64_t)kPrefillFp4Cols * (cfg.head_dim + 2) * 4;
+    const int64_t places = 3 * (int64_t)std::max(h->num_cus, 1) - p.append_blocks, part_bytes = (int64_t)kPrefillFp4Cols * (cfg.head_dim + 2) * 4;
     int64_t ranges = std::max<int64_t>(1, places / p.Hkv);
     ranges = std::min<int64_t>(ranges, (int64_t)(2 * h->scratch_units * h->unit_bytes) / (2 * part_bytes * p.Hkv));
     ranges = std::min<int64_t>(ranges, h->n_counters / p.Hkv);
@@ -1000,12 +977,22 @@ static bool plan_small_tiles(const tetri_ctx *h, int32_t num_segs, bool append, 
     return ranges >= 1 && tiles * ((int64_t)p.max_blocks / 2 + p.C / 32 + 8) <= 0x7fffffff && (columns + kPrefillFp4Cols) * p.g < 0xffffffffll &&
            ranges * p.Hkv * p.Hkv < 0xffffffffll;
 }
-// Whether a chunk goes there.
+// Whether a chunk goes there.  The other kernel's tiles are 128 columns (32 to 128 rows) and 64 or 128 keys: twice the rate on full tiles, but most of a tile is idle
+// behind a short segment.
+//  - Heads of 128: chunks of many short segments, whose tiles are filled to a sixth on average and are four fifths of the compute units or more.  (256 rows of 40 heads in
+//    32 segments without context 24 us, the other kernel 44, behind 0 to 4000 tokens 121 and 231; 256 rows of 32 heads over 8 in 64 segments 18.7 and
+//    19.5, 65 and 133; but in 32 segments, filled to a fifth, 16.1 and 12.2 without context, 44 and 67 with; one segment of 512 rows 44 and 19.5.)
+//  - Heads of 64, where everything of a wavefront is in registers: as long as a chunk has no more columns than half the chip's tiles.  (256 rows of 6 heads over 2
+//    behind 4000 tokens 22 and 36 us, without context 8.9 and 11.8; 2048 rows 44 and 88, 26 and 39; 8 short segments of 1024 rows 25 and 11, behind 0 to 4000 tokens
+//    36 and 46.)
 static bool small_tiles_preferred(const tetri_ctx *h, int32_t num_segs)
 {
-    (void)h;
-    (void)num_segs;
-    return true;
+    int hpw, rb;
+    wave_grouping(h->cfg.num_q_heads / h->cfg.num_kv_heads, 4, &hpw, &rb);
+    const int64_t groups = h->cfg.num_q_heads / hpw, full = h->cfg.chunk_size * groups / (32 * rb), cus = std::max(h->num_cus, 1);
+    if (h->cfg.head_dim == 64) return 2 * full <= cus;
+    const int64_t bound = groups * tile_bound(h->cfg.chunk_size, num_segs, 32 * rb);
+    return 5 * bound >= 4 * cus && 6 * full <= bound;
 }
 
 static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new,
@@ -1013,7 +1000,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
                                 const int32_t *ctx_lens, int32_t num_segs, float scale, void *out, void *stream,
                                 bool fp8 = false, float k_scale = 1.f, float v_scale = 1.f,
                                 const int32_t *host_cu = nullptr, const int32_t *host_ctx = nullptr, MetaUpload *carry = nullptr,
-                                const NextRows *next = nullptr, bool fp4 = false)
+                                const NextRows *next = nullptr, const Fp4Launchers *fp4 = nullptr)
 {
     const void *ptrs[] = {q, k_new, v_new, kv_pages, out};
     const char *names[] = {"q", "k_new", "v_new", "kv_pages", "out"};
@@ -1093,7 +1080,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
         const CounterSets cs = counter_sets(h->counters, h->n_counters, h->counter_turn);
         fp.counters = cs.use;
         fp.counters_next = cs.clear;
-        hipError_t e = tetri_launch_prefill_fp4(h->cfg.head_dim, fp, hs);
+        hipError_t e = fp4->prefill(h->cfg.head_dim, fp, hs);
         if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
         ++h->counter_turn;
         if (!capturing) scratch_claimed(h, hs);
@@ -1144,7 +1131,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
             p.counters = cs.use;
             p.counters_next = cs.clear;
             plan.done = plan.places != 0 && mem == 1 ? h->plan_done : nullptr;
-            hipError_t e = tetri_launch_attn(h, p, 2, fp8 ? 8 : 16, hs);
+            hipError_t e = tetri_launch_attn(h, p, 2, fp8, hs);
             if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
             if (plan.places != 0) plan_memory_used(h, mem, hs);
             return TETRI_OK;
@@ -1176,17 +1163,27 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
     // stream mode at most 64 segments (one lane each) and positions times G in 31 bits.
     int G = 0;
     p.helpers = 0;
+    // Workgroups that take the chunk's rows to their slots beside a stream: rows that become 4-bit codes need more of them than the eight that
+    // copy (1024 rows of 8 heads over 2: 28 us with eight).
+    const int code_append = fp4 && kv_pages_w ? std::max(8, std::min(32, p.C / 512 * 8)) : 0;
     const bool counters_fit = (int64_t)groups * p.tiles * 4 <= h->n_counters;
     if (h->stream_wgs > 0) {
         G = h->stream_wgs;
     } else if (h->split_keys) {
         const int helpers = p.tiles / 2 + 1;
         // (the last tile of the bound and its helper exist only in chunks with ragged segments and are not counted)
-        if (p.tiles >= 2 && (int64_t)(p.tiles - 1 + helpers - 1) * groups <= cus && (size_t)p.tiles * groups * 4 <= h->scratch_units)
+        const int64_t jobs = (int64_t)(p.tiles - 1 + helpers - 1) * groups;
+        const bool long_segs = (int64_t)p.C >= 256 * (int64_t)p.S, streams = (key_parts == 2 || h->attn_variant == 1) && (int64_t)p.tiles * groups < 2 * (int64_t)cus;
+        // Over 4-bit codes, where contexts are long, stream mode also takes what tail mode would run on four fifths of the compute units or fewer (256 rows of 32 heads
+        // over 8: behind 16000 tokens 98 us, with tails 191, behind 3000 42 and 55, without any 14.6 and 14.7) and chunks of short segments (512 rows of the same
+        // heads in 7 segments behind 0 to 3000 tokens 55.8 and 64.9, 20 behind 0 to 6000 76 and 96; 20 without any 16.7 and 12.6).
+        if (fp4 && streams && !(p.tiles >= 2 && long_segs && jobs <= cus && 5 * jobs > 4 * (int64_t)cus))
+            G = std::min(255, (cus - code_append) / groups);
+        else if (p.tiles >= 2 && jobs <= cus && (size_t)p.tiles * groups * 4 <= h->scratch_units)
             p.helpers = helpers;
         // (segments of under 256 rows on average are a batch of short prompts: a handful of stages per tile, which
         // the division would only cut into smaller pieces)
-        else if ((key_parts == 2 || h->attn_variant == 1) && (int64_t)p.tiles * groups < 2 * (int64_t)cus && (int64_t)p.C >= 256 * (int64_t)p.S)
+        else if (streams && long_segs)
             G = std::min(255, (cus - (kv_pages_w ? 8 : 0)) / groups);
     }
     const int stage = 64 * key_parts;
@@ -1209,7 +1206,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
     int append_wgs = 64;
     if (shares) {
         const int idle = cus - p.attn_first;
-        append_wgs = idle >= 8 ? (idle < 64 ? idle / 8 * 8 : 64) : 8;
+        append_wgs = G > 0 && code_append > 0 ? std::max(code_append, std::min(64, idle / 8 * 8)) : idle >= 8 ? (idle < 64 ? idle / 8 * 8 : 64) : 8;
     }
     p.append_blocks = kv_pages_w ? (p.C < append_wgs ? p.C : append_wgs) : 0;
     p.hpw_shift = log2i(p.hpw);
@@ -1227,7 +1224,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
     p.kv_magic = magic((uint32_t)(p.g / p.hpw));
     if ((uint64_t)p.attn_grid * (uint64_t)(p.tiles + G + 1) >= 0x100000000ull)
         return fail(h, TETRI_ERR_UNSUPPORTED, "%s: chunk_size x heads too large for one launch", fn);
-    hipError_t e = tetri_launch_attn(h, p, key_parts, fp4 ? 4 : (fp8 ? 8 : 16), hs);
+    hipError_t e = fp4 ? fp4->attn(h, p, key_parts, hs) : tetri_launch_attn(h, p, key_parts, fp8, hs);
     if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
     if (shares) {
         ++h->counter_turn;
@@ -1261,83 +1258,6 @@ tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *h, const void *q, const voi
     if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_chunk_prefill_attn_fp8: append must be 0 or 1");
     return attn_common("tetri_chunk_prefill_attn_fp8", h, q, k_new, v_new, kv_pages_fp8, append ? kv_pages_fp8 : nullptr,
                        block_table, cu, ctx_lens, num_segs, scale, out, stream, true, k_scale, v_scale);
-}
-
-tetri_status tetri_chunk_prefill_attn_fp4(tetri_ctx *h, const void *q, const void *k_new, const void *v_new, void *kv_pages_fp4,
-                                          const int32_t *block_table, const int32_t *cu, const int32_t *ctx_lens, int32_t num_segs, float scale,
-                                          int32_t append, void *out, void *stream)
-{
-    if (append != 0 && append != 1) return fail(h, TETRI_ERR_INVALID_ARG, "tetri_chunk_prefill_attn_fp4: append must be 0 or 1");
-    return attn_common("tetri_chunk_prefill_attn_fp4", h, q, k_new, v_new, kv_pages_fp4, append ? kv_pages_fp4 : nullptr, block_table, cu, ctx_lens,
-                       num_segs, scale, out, stream, false, 1.f, 1.f, nullptr, nullptr, nullptr, nullptr, true);
-}
-
-tetri_status tetri_qk_norm_rope(tetri_ctx *h, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_weight,
-                                const void *k_weight, float eps, const tetri_rope *rope, const int32_t *positions, const int32_t *cu,
-                                const int32_t *ctx_lens, int32_t num_segs, int32_t num_rows, void *q_out, void *k_out, void *stream)
-{
-    const char *fn = "tetri_qk_norm_rope";
-    if (!h) return fail(nullptr, TETRI_ERR_INVALID_ARG, "%s: null handle", fn);
-    const void *ptrs[] = {q, k, q_out, k_out};
-    const char *names[] = {"q", "k", "q_out", "k_out"};
-    for (int i = 0; i < 4; ++i) {
-        if (!ptrs[i]) return fail(h, TETRI_ERR_INVALID_ARG, "%s: %s is null", fn, names[i]);
-        if (!aligned16(ptrs[i])) return fail(h, TETRI_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", fn, names[i]);
-    }
-    if (!aligned16(q_weight) || !aligned16(k_weight)) return fail(h, TETRI_ERR_INVALID_ARG, "%s: q_weight or k_weight is not 16-byte aligned", fn);
-    const tetri_config &cfg = h->cfg;
-    const int64_t q_row = (int64_t)cfg.num_q_heads * cfg.head_dim, k_row = (int64_t)cfg.num_kv_heads * cfg.head_dim;
-    if (q_stride < q_row || k_stride < k_row || q_stride % 8 != 0 || k_stride % 8 != 0 || q_stride > (1ll << 40) || k_stride > (1ll << 40))
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: q_stride=%lld and k_stride=%lld have to be multiples of 8, at least %lld and %lld", fn,
-                    (long long)q_stride, (long long)k_stride, (long long)q_row, (long long)k_row);
-    if ((q_out == q && q_stride != q_row) || (k_out == k && k_stride != k_row))
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: in place only where the rows follow each other", fn);
-    if (!(std::isfinite(eps) && eps >= 0.f)) return fail(h, TETRI_ERR_INVALID_ARG, "%s: eps is negative or not finite", fn);
-    if (!rope) return fail(h, TETRI_ERR_INVALID_ARG, "%s: rope is null", fn);
-    if (rope->num_pairs < 8 || rope->num_pairs > cfg.head_dim / 2 || rope->num_pairs % 8 != 0)
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_pairs=%d is no multiple of 8 in 8..%d", fn, rope->num_pairs, cfg.head_dim / 2);
-    if (rope->num_axes < 1 || rope->num_axes > 8) return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_axes=%d outside 1..8", fn, rope->num_axes);
-    if (rope->adjacent != 0 && rope->adjacent != 1) return fail(h, TETRI_ERR_INVALID_ARG, "%s: adjacent must be 0 or 1", fn);
-    if (num_rows < 1) return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_rows=%d is not positive", fn, num_rows);
-    if (positions ? (cu || ctx_lens) : !(cu && ctx_lens))
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: either positions or cu_chunk_q_lens and ctx_lens", fn);
-    if (cu && (num_segs < 1 || num_segs > cfg.max_segs_per_chunk))
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: num_segs=%d outside 1..%d", fn, num_segs, cfg.max_segs_per_chunk);
-    RopeParams p;
-    for (int i = 0; i < TETRI_ROPE_PAIRS; ++i) {
-        const bool used = i < rope->num_pairs;
-        p.freq[i] = used ? rope->freq[i] : 0.f;
-        p.axis[i] = used ? rope->axis[i] : 0;
-        if (!std::isfinite(p.freq[i])) return fail(h, TETRI_ERR_INVALID_ARG, "%s: freq[%d] is not finite", fn, i);
-        if (p.axis[i] >= rope->num_axes) return fail(h, TETRI_ERR_INVALID_ARG, "%s: axis[%d]=%d of %d axes", fn, i, p.axis[i], rope->num_axes);
-    }
-    int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev != h->device)
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: the handle was created on device %d, the current device is %d", fn, h->device, dev);
-    p.q = static_cast<const uint16_t *>(q); p.k = static_cast<const uint16_t *>(k);
-    p.q_weight = static_cast<const uint16_t *>(q_weight); p.k_weight = static_cast<const uint16_t *>(k_weight);
-    p.q_out = static_cast<uint16_t *>(q_out); p.k_out = static_cast<uint16_t *>(k_out);
-    p.pos = positions; p.cu = cu; p.ctx = ctx_lens;
-    p.q_stride = q_stride; p.k_stride = k_stride;
-    p.eps = eps;
-    p.S = num_segs; p.rows = num_rows; p.Hq = cfg.num_q_heads; p.Hkv = cfg.num_kv_heads;
-    p.pairs = rope->num_pairs; p.adjacent = rope->adjacent;
-    // A row's heads go to one wavefront where rows are many (its cosines and sines are worked out once), otherwise to as many as fill eight places of
-    // a compute unit, down to the heads of one instruction each.
-    const int64_t per_inst = 512 / cfg.head_dim, insts = (p.Hq + p.Hkv + per_inst - 1) / per_inst;
-    const int64_t want = std::max<int64_t>(1, std::min(insts, 8 * (int64_t)std::max(h->num_cus, 1) / num_rows));
-    p.per_split = (int32_t)((insts + want - 1) / want);
-    p.splits = (int32_t)((insts + p.per_split - 1) / p.per_split);
-    p.splits_magic = p.splits <= 1 ? 0u : (uint32_t)((0x100000000ull + p.splits - 1) / p.splits);
-    // More than 64 MB of rows: read past the caches, where what is written then finds room, and what is read next.  (8192 rows of 32/8 heads 38.6 -> 32.7 us, with
-    // the chunk's attention behind it 116.9 -> 115.0; but 512 rows of 40 heads 7.3 and 7.9, with attention 31.1 and 32.0.  Writing past the caches is faster alone, 32.1
-    // and 6.4, and slower with the attention that reads it: 121.3.)
-    p.past_caches = (q_row + k_row) * 2 * num_rows > (64ll << 20);
-    if ((uint64_t)num_rows * p.splits * p.splits + 4ull * p.splits >= 0x7fffffffull)
-        return fail(h, TETRI_ERR_INVALID_ARG, "%s: too many rows for one launch", fn);
-    hipError_t e = tetri_launch_rope(cfg.head_dim, p, static_cast<hipStream_t>(stream));
-    if (e != hipSuccess) return fail(h, TETRI_ERR_HIP, "%s: launch failed: %s", fn, hipGetErrorString(e));
-    return TETRI_OK;
 }
 
 // Host copies of a chunk's metadata: are they a chunk of this handle?
@@ -1601,4 +1521,28 @@ tetri_status tetri_decode_call(const char *fn, tetri_ctx *h, const void *q, cons
 {
     return decode_common(fn, h, q, k_new, v_new, kv_pages, kv_pages_w, block_table, ctx_lens, num_reqs, max_ctx_len, scale, out, stream, fp8, k_scale,
                          v_scale, false, weights);
+}
+
+tetri_status tetri_transfer_fp4_call(const char *fn, tetri_ctx *h, void *kv_pages, void *buf, const int32_t *block_table, const int32_t *cu_tokens,
+                                     const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, bool to_pool, void *stream,
+                                     const Fp4Launchers &fp4)
+{
+    return kv_transfer(fn, h, kv_pages, buf, block_table, cu_tokens, first_tokens, num_reqs, total_tokens, to_pool, stream, to_pool ? 4 : 3, 1.f, 1.f,
+                       &fp4);
+}
+
+tetri_status tetri_decode_fp4_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages,
+                                   void *kv_pages_w, const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len,
+                                   float scale, void *out, void *stream, const Fp4Launchers &fp4)
+{
+    return decode_common(fn, h, q, k_new, v_new, kv_pages, kv_pages_w, block_table, ctx_lens, num_reqs, max_ctx_len, scale, out, stream, false, 1.f,
+                         1.f, false, nullptr, &fp4);
+}
+
+tetri_status tetri_prefill_fp4_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages,
+                                    void *kv_pages_w, const int32_t *block_table, const int32_t *cu, const int32_t *ctx_lens, int32_t num_segs,
+                                    float scale, void *out, void *stream, const Fp4Launchers &fp4)
+{
+    return attn_common(fn, h, q, k_new, v_new, kv_pages, kv_pages_w, block_table, cu, ctx_lens, num_segs, scale, out, stream, false, 1.f, 1.f, nullptr,
+                       nullptr, nullptr, nullptr, &fp4);
 }

@@ -355,7 +355,7 @@ struct CompactParams {
     int32_t B, Hkv, max_blocks, keep, recent;
 };
 
-// Prefill over a pool of 4-bit codes in tiles of 32 columns (tetri_prefill_fp4.hip).
+// Prefill over a pool of 4-bit codes in tiles of so many columns (tetri_prefill_fp4.hip).
 constexpr int32_t kPrefillFp4Cols = 32;
 struct PrefillFp4Params {
     const uint16_t *q, *k_new, *v_new, *pages;
@@ -394,8 +394,8 @@ struct RopeParams {
     uint8_t axis[TETRI_ROPE_PAIRS];
 };
 
-// pool_bits: of an element of the pool, 16, 8 (E4M3 codes) or 4 (microscaled E2M1 codes; not for p.plan)
-hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, int pool_bits, hipStream_t stream);
+hipError_t tetri_launch_attn(const tetri_ctx *h, const AttnParams &p, int key_parts, bool fp8_pool, hipStream_t stream);
+hipError_t tetri_launch_attn_fp4(const tetri_ctx *h, const AttnParams &p, int key_parts, hipStream_t stream);       // a pool of 4-bit codes; not for p.plan
 hipError_t tetri_launch_planned(const AttnParams &p, bool fp8_pool, hipStream_t stream);      // (tetri_launch_attn's, for p.plan)
 hipError_t tetri_launch_short(int head_dim, bool fp8_pool, const ShortParams &p, int wavefronts, hipStream_t stream);
 hipError_t tetri_launch_kv_transfer(const tetri_ctx *h, const TransferParams &p, int32_t row_units, int32_t tiles,
@@ -421,6 +421,23 @@ tetri_status tetri_fail(tetri_ctx *h, tetri_status st, const char *fmt, ...) __a
 tetri_status tetri_decode_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages, void *kv_pages_w,
                                const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len, float scale, void *out,
                                void *stream, bool fp8, float k_scale, float v_scale, const DecodeWeights *weights);
+// Kernels over 4-bit codes, handed to the shared host layer by the entry points that have them (tetri_fp4_host.cpp).
+struct Fp4Launchers {
+    hipError_t (*export_codes)(const tetri_ctx *, const TransferParams &, int32_t tiles, hipStream_t);
+    hipError_t (*import_codes)(const tetri_ctx *, const TransferParams &, int32_t tiles, hipStream_t);
+    hipError_t (*decode)(const tetri_ctx *, const DecodeParams &, hipStream_t);
+    hipError_t (*attn)(const tetri_ctx *, const AttnParams &, int key_parts, hipStream_t);
+    hipError_t (*prefill)(int head_dim, const PrefillFp4Params &, hipStream_t);
+};
+tetri_status tetri_transfer_fp4_call(const char *fn, tetri_ctx *h, void *kv_pages, void *buf, const int32_t *block_table, const int32_t *cu_tokens,
+                                     const int32_t *first_tokens, int32_t num_reqs, int64_t total_tokens, bool to_pool, void *stream,
+                                     const Fp4Launchers &fp4);
+tetri_status tetri_decode_fp4_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages,
+                                   void *kv_pages_w, const int32_t *block_table, const int32_t *ctx_lens, int32_t num_reqs, int32_t max_ctx_len,
+                                   float scale, void *out, void *stream, const Fp4Launchers &fp4);
+tetri_status tetri_prefill_fp4_call(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new, const void *kv_pages,
+                                    void *kv_pages_w, const int32_t *block_table, const int32_t *cu, const int32_t *ctx_lens, int32_t num_segs,
+                                    float scale, void *out, void *stream, const Fp4Launchers &fp4);
 
 // Copies len int32 (rounded up to a multiple of 4) from pinned host memory to the device, both 16-byte aligned; `done` (null:
 // none) is signalled when that has ended.

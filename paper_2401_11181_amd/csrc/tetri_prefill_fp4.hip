@@ -2,15 +2,19 @@
 // workgroup, which then walks all keys, 128 at a time, behind barriers; here a tile is a quarter as large and any number of workgroups share its keys.
 //
 //   * A tile is 32 columns of one kv head: neighbouring (row, query head of the kv head) pairs of a segment, rows first, so that codes become bf16
-//     once for all heads that share them.  A wavefront takes whole steps of 32 keys by itself (fp4_steps.h), from a ring in LDS; no barrier
-//     stands between steps.  The chunk's own rows are steps as well, of bf16 rows that go straight into registers.
+//     once for all heads that share them.  A wavefront takes whole steps of 32 keys by itself (fp4_steps.h), from a ring in LDS, for all of the
+//     tile's columns; no barrier stands between steps, and a step's codes are on their way from LDS while the one before it is made.  The
+//     chunk's own rows are steps as well, of bf16 rows that go straight into registers.
 //   * The steps of all tiles of a kv head, tile after tile, are cut into equal ranges, a workgroup each, worked out on the device from the
 //     segments' lengths, the same for every kv head.  A tile counts with all new rows of its segment, whatever its rows see of them, and with
-//     kTileSteps more.  The wavefronts of a workgroup take a tile's steps in turn and merge in LDS when it is done.
+//     kTileSteps more.  The wavefronts of a workgroup take a tile's steps in turn; when it is done every one of them gets a quarter of the others'
+//     accumulators, as they lie in registers, through LDS.
 //   * Tiles cut between workgroups meet through arrival counters in the same launch, as in tetri_decode.hip: the workgroup that arrives last merges the
 //     parts in their order.  Nobody waits.
 //   * Workgroups of a kv head run on one XCD (or two, four, eight where there are few kv heads): tiles of a segment read the same keys through its L2.
 //   * The chunk's rows are cached in codes by a few workgroups in front of the others; padding rows of the output are zeroed by all.
+#include <type_traits>
+
 #include "fp4_steps.h"
 
 namespace {
@@ -19,13 +23,10 @@ using namespace tetri_dev;
 
 constexpr int kWaves = 4;         // wavefronts of a workgroup
 constexpr int kDepth = 2;         // steps a wavefront's ring holds
-constexpr int kNB = 2;            // blocks of 16 columns
-constexpr int kCols = 16 * kNB;
-constexpr int kMergeCols = 8;     // columns whose partial O the merge area in LDS holds at a time
+constexpr int kNB = 2, kCols = 16 * kNB;        // columns of a tile
 constexpr int kTileSteps = 4;     // what a tile costs a range beside its steps, in steps
-constexpr int kBatch = 64;        // parts whose weights the merge of a cut tile holds at a time
 
-// A workgroup's partial result: O of the columns (unnormalised), their m, their row sums.
+// A workgroup's partial result: its accumulators as they lie in registers (a vector of 4 per product and lane), then m and the row sum of the columns.
 template <int D> constexpr int kPartFloats = kCols * (D + 2);
 
 // A stretch of steps of one tile; wave-uniform.
@@ -66,6 +67,13 @@ template <int D> struct NewRows {
             }
         }
     }
+    __device__ __forceinline__ void negate_k()
+    {
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kw[pg][s] ^= 0x80008000u;
+    }
     __device__ __forceinline__ bf16x8 k(int pg, int s) const { return __builtin_bit_cast(bf16x8, kw[pg][s]); }
     template <int T> __device__ __forceinline__ uint32_t v(int x) const { return vw[x][T]; }
 };
@@ -94,13 +102,21 @@ template <int D> __device__ __forceinline__ void append_rows(const PrefillFp4Par
     }
 }
 
+// Three workgroups to a compute unit.  What bounds it is the vector unit: a step of 32 keys and 32 columns is 32 matrix instructions (about 16 clocks each) beside some
+// 160 others, and at heads of 128 the registers of a third of a SIMD do not hold everything: Q is read from LDS at every step, and values of a tile that steps do not need go to
+// scratch memory.  (With two workgroups, Q in registers and three steps in a ring, nothing in scratch: 512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens
+// 65.9 us, 64.3 so; 256 of 8 over 2 behind 8000 43.0 and 41.3; 128 of 40 behind 0 to 4000 38.2 and 32.3.  Tiles of 64 columns: 65.0, 74.6 and 36.)
 template <int D>
-__global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4Params p)
+__global__ __launch_bounds__(kWaves * 64, 3) void prefill_fp4_kernel(PrefillFp4Params p)
 {
     typedef Step<D> T;
-    constexpr int NW = kWaves, NT = NW * 64, NB = kNB;
+    constexpr int NW = kWaves, NT = NW * 64, KS = D / 32, DJ = D / 16, NB = kNB;
+    constexpr int UNITS = NB * DJ / NW;                  // accumulators of a wavefront's quarter: products j0 .. of block nb
+    static_assert(DJ % UNITS == 0, "of one block");
     __shared__ __attribute__((aligned(1024))) char smem[NW * kDepth * T::BYTES];
-    __shared__ __attribute__((aligned(16))) float area[NW][kMergeCols][D];
+    // Q's fragments, [block][s][lane] of 16 bytes, while a tile's steps are made; then what the wavefronts hand each other, [wavefront][unit][lane]
+    __shared__ __attribute__((aligned(1024))) char area[NW * UNITS * 1024];
+    static_assert(NB * KS * 1024 <= (int)sizeof(area), "Q's fragments");
     __shared__ float stat[NW][2][kCols];
     __shared__ int arrived[2];
     const int tid = threadIdx.x, lane = tid & 63;
@@ -214,6 +230,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4P
     const uint32_t my_lds = lds_address(my);
     const StepSource<D> source(lane, v_delta);
 
+    // ---- Q's fragments: columns past the tile's end repeat the last one, their results are not stored
+    const uint32_t area_lds = lds_address(area);
+    auto load_q = [&](const Job &j) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int col = min(kCols * j.t + 16 * nb + l16, j.n * g - 1), r = magic_div(col, p.g_magic);
+            const uint16_t *src = p.q + ((size_t)(j.row0 + r) * p.Hq + (size_t)kh * g + (col - r * g)) * D + grp * (D / 4);
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                if ((nb * KS + s) % NW == wave) dma16(src + 8 * s, area_lds + (nb * KS + s) * 1024);
+        }
+    };
+    load_q(job);
+
     // ---- the wavefront's cursor over steps of cached keys: step fs of job fj goes next (fs < 0: there is none), the page ids of it and the 31 behind it
     // are in the lanes of `ids`
     Job fj = job;
@@ -229,101 +259,111 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4P
             const int n = (fj.L + kPage - 1) / kPage, e = 2 * (fs + NW * (lane >> 1)) + (lane & 1);
             ids = 0;
             if (e < n) ids = reinterpret_cast<__attribute__((address_space(1))) const int32_t *>((uintptr_t)(p.bt + (size_t)fj.s * p.max_blocks))[e];
+            wait_vm<0>();                                // (here, once in 32 steps: the compiler's own wait stands at every step, where it drains the loads in flight)
             id_at = 0;
         }
     };
-    auto issue = [&](int place) {
+    // steps in flight; the first one's K is on its way into registers
+    int many = 0;
+    uint32_t place_in = 0, place_out = 0;                // bytes
+    auto turn = [](uint32_t &place) { place = place == (kDepth - 1) * T::BYTES ? 0 : place + T::BYTES; };
+    auto issue = [&]() {
         const int pg0 = __builtin_amdgcn_readlane(ids, id_at), pg1 = __builtin_amdgcn_readlane(ids, id_at + 1);
         id_at += 2;
-        issue_step<D>(source, pool + (size_t)pg0 * page_bytes, pool + (size_t)pg1 * page_bytes, v_delta, lane, my_lds + place * T::BYTES);
+        issue_step<D, false>(source, pool + (size_t)pg0 * page_bytes, pool + (size_t)pg1 * page_bytes, v_delta, lane, my_lds + place_in);
+        turn(place_in);
+        ++many;
+        fs += NW;
+        settle();
     };
-    int ahead = 0, rj[kDepth], rs[kDepth], place_in = 0, place_out = 0;
+    auto lds_reads_done = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(15 | 3 << 14 | 7 << 4);           // (vector memory is not waited for)
+        asm volatile("" ::: "memory");
+    };
+    StepCodes<D> codes;
     settle();
-#pragma unroll
-    for (int i = 0; i < kDepth; ++i) {
-        rj[i] = 0; rs[i] = -1;
-        if (fs >= 0) {
-            issue(place_in);
-            if (++place_in == kDepth) place_in = 0;
-            rj[i] = fj.seq; rs[i] = fs;
-            ++ahead;
-            fs += NW;
-            settle();
-        }
-    }
+    if (fs >= 0) issue();
+    const bool any = many != 0;
+    if (fs >= 0) issue();
+    static_assert(kDepth == 2, "the first loads, and waits for what is in flight");
+    if (many == 2) wait_vm<T::LOADS>();
+    else wait_vm<0>();
+    if (any) codes.read_k(my, grp, l16);
 
     // What this workgroup has left of tiles cut between workgroups, two at most: where their rows are, arrival counter, parts and where they are.
     int cut_row0[2], cut_n[2], cut_t[2], cut_counter[2], cut_pieces[2], cut_w0[2], cuts = 0;
     auto place_of = [&](int w0, int i) -> float * { return p.scratch + ((size_t)(2 * (w0 + i) + (int)(i == 0)) * p.Hkv + kh) * kPartFloats<D>; };
-    auto out_of = [&](int row0, int col) -> uint16_t * {
-        const int r = magic_div(col, p.g_magic);
-        return p.out + ((size_t)(row0 + r) * p.Hq + (size_t)kh * g + (col - r * g)) * D;
-    };
-    auto write_pair = [&](uint16_t *to, float a, float b, float inv) {
-        bf16x2 r;
-        r[0] = (__bf16)(a * inv);
-        r[1] = (__bf16)(b * inv);
-        *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)to) = __builtin_bit_cast(uint32_t, r);
+    const int my_nb = wave * UNITS / DJ, my_j = wave * UNITS % DJ;       // the wavefront's quarter
+    // the wavefront's quarter of a finished tile: row 4 * grp + i of product j is d = DJ * (4 * grp + i) + j
+    auto write_quarter = [&](int row0, int t, int cols, const f32x4 (&o)[UNITS], float inv) {
+        const int col = 16 * my_nb + l16;
+        if (col >= cols) return;
+        const int all = kCols * t + col, r = magic_div(all, p.g_magic);
+        uint16_t *to = p.out + ((size_t)(row0 + r) * p.Hq + (size_t)kh * g + (all - r * g)) * D + my_j;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t w[UNITS / 2];
+#pragma unroll
+            for (int u = 0; u < UNITS; u += 2) {
+                bf16x2 y;
+                y[0] = (__bf16)(o[u][i] * inv);
+                y[1] = (__bf16)(o[u + 1][i] * inv);
+                w[u / 2] = __builtin_bit_cast(uint32_t, y);
+            }
+            uint16_t *at = to + DJ * (4 * grp + i);
+            if constexpr (UNITS == 8) *reinterpret_cast<global_u32x4_w *>((uintptr_t)at) = u32x4{w[0], w[1], w[2], w[3]};
+            else if constexpr (UNITS == 4) *reinterpret_cast<global_u32x2_w *>((uintptr_t)at) = u32x2{w[0], w[1]};
+            else *reinterpret_cast<__attribute__((address_space(1))) uint32_t *>((uintptr_t)at) = w[0];
+        }
     };
     const float c = p.c;
+    const bool neg = p.neg != 0;
     Columns<D, NB> x;
+    auto q_of = [&](int nb, int s) -> bf16x8 { return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(area + (nb * KS + s) * 1024 + lane * 16)); };
 
+    lds_barrier();                                       // (everybody's part of Q is older than a wavefront's first step)
     for (;;) {                                           // the jobs of the range
         x.clear();
         int row_of[NB];                                  // the row of the lane's column
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const int col = min(kCols * job.t + 16 * nb + l16, job.n * g - 1);       // (columns past the end repeat the last one: their results are not stored)
-            row_of[nb] = magic_div(col, p.g_magic);
-            const global_u32x4 *qp = reinterpret_cast<const global_u32x4 *>((uintptr_t)(p.q + ((size_t)(job.row0 + row_of[nb]) * p.Hq + (size_t)kh * g + (col - row_of[nb] * g)) * D
-                                                                                        + grp * (D / 4)));
-#pragma unroll
-            for (int s = 0; s < D / 32; ++s) {
-                u32x4 v = u32x4(qp[s]);
-                if (p.neg) v ^= 0x80008000u;             // (a negative scale is Q's sign)
-                x.qf[nb][s] = __builtin_bit_cast(bf16x8, v);
-            }
-        }
-        // ---- cached keys
-        while (rs[0] >= 0 && rj[0] == job.seq) {
-            const int cs = rs[0];
-            if (ahead == 1) wait_vm<0>();
-            else wait_vm<T::LOADS>();
-            static_assert(kDepth == 2, "a wait for one step behind the current one");
-            StepCodes<D> codes;
-            codes.read(my + place_out * T::BYTES, grp, l16);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // everything is in registers: the place may be overwritten
-            const bool far = fs >= 0;
-            if (far) issue(place_in);
-            if (++place_out == kDepth) place_out = 0;
-            codes.powers(l16);
+        for (int nb = 0; nb < NB; ++nb) row_of[nb] = magic_div(min(kCols * job.t + 16 * nb + l16, job.n * g - 1), p.g_magic);
+        // ---- cached keys.  A step: K's codes have arrived, V's are asked for; behind the scores the next step's K; behind the weights the place is free
+        // for the loads of the last step behind it
+        for (int cs = job.begin + wave; cs < min(job.end, job.cached); cs += NW) {
+            lds_reads_done();
+            codes.read_v(my + place_out, grp, l16);
+            if (neg) codes.negate_k();
             f32x4 sc[NB][2];
-            x.scores(codes, sc);
-            if (32 * cs + 32 > job.L) {                  // slots past the end are masked
-                const int n = job.L - 32 * cs;
+            x.scores(codes, q_of, sc);
+            --many;
+            turn(place_out);
+            if (many > 0) {
+                wait_vm<0>();
+                codes.read_k(my + place_out, grp, l16);
+            }
+            const int n = job.L - 32 * cs;               // slots past the end are masked
+            if (n < 32) {
 #pragma unroll
                 for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (16 * pg + 4 * i + grp >= n) {
-                            codes.vs[4 * pg + i] = 0.f;
 #pragma unroll
                             for (int nb = 0; nb < NB; ++nb) sc[nb][pg][i] = -INFINITY;
                         }
             }
             bf16x8 pf[NB];
             x.weigh(sc, c, pf);
-            x.add(codes, pf);
-            rj[0] = rj[1]; rs[0] = rs[1];
-            rs[1] = -1;
-            --ahead;
-            if (far) {
-                rj[1] = fj.seq; rs[1] = fs;
-                ++ahead;
-                if (++place_in == kDepth) place_in = 0;
-                fs += NW;
-                settle();
+            lds_reads_done();
+            if (fs >= 0) issue();
+            codes.powers(l16);
+            if (n < 32) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (16 * (i / 4) + 4 * (i % 4) + grp >= n) codes.vs[i] = 0.f;
             }
+            x.add(codes, pf);
         }
         // ---- the chunk's own rows
         {
@@ -335,8 +375,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4P
                 const int first = 32 * (s - job.cached);
                 NewRows<D> rows;
                 rows.load(p.k_new + at, p.v_new + at, row_elements, first, seen, grp, l16);
+                if (neg) rows.negate_k();
                 f32x4 sc[NB][2];
-                x.scores(rows, sc);
+                x.scores(rows, q_of, sc);
 #pragma unroll
                 for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
@@ -350,62 +391,78 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4P
             }
         }
         // ---- the job is done: the wavefronts merge
+        Job after = job;
+        int after_pos = pos;
+        const bool more = left != 0 && (next_job(after, left, after_pos), after.end != 0);
         const bool whole = job.begin == 0 && job.end == job.steps;
+        const int cols = min(kCols, job.n * g - kCols * job.t);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
             if (grp == 0) { stat[wave][0][16 * nb + l16] = x.m[nb]; stat[wave][1][16 * nb + l16] = x.lsum[nb][0]; }
-        int piece = 0, w0 = 0;
-        if (!whole) {
+        lds_barrier();                                   // (also: everybody is done with Q)
+        const int my_col = 16 * my_nb + l16;
+        float top = stat[0][0][my_col], sum = 0.f;
+#pragma unroll
+        for (int i = 1; i < NW; ++i) top = fmaxf(top, stat[i][0][my_col]);
+#pragma unroll
+        for (int i = 0; i < NW; ++i) sum = __builtin_fmaf(stat[i][1][my_col], __builtin_amdgcn_exp2f(stat[i][0][my_col] - top), sum);
+        f32x4 mine[UNITS];
+        auto each_quarter = [&](int which, auto &&f) {   // f with the accumulators of quarter `which` (registers have no computed index)
+            auto of = [&](auto w) {
+                constexpr int U = decltype(w)::value * UNITS;
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) f(u, x.o[U / DJ][U % DJ + u]);
+            };
+            switch (which) {
+            case 0: of(std::integral_constant<int, 0>()); break;
+            case 1: of(std::integral_constant<int, 1>()); break;
+            case 2: of(std::integral_constant<int, 2>()); break;
+            default: of(std::integral_constant<int, 3>()); break;
+            }
+        };
+        {
+            const float w = __builtin_amdgcn_exp2f(stat[wave][0][my_col] - top);
+            each_quarter(wave, [&](int u, const f32x4 &o) { mine[u] = o * w; });
+        }
+#pragma unroll 1
+        for (int r = 1; r < NW; ++r) {
+            if (r != 1) lds_barrier();                   // everybody has read the round before
+            each_quarter(wave ^ r, [&](int u, const f32x4 &o) { *reinterpret_cast<f32x4 *>(area + (wave * UNITS + u) * 1024 + lane * 16) = o; });
+            lds_barrier();
+            const float w = __builtin_amdgcn_exp2f(stat[wave ^ r][0][my_col] - top);
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const f32x4 z = *reinterpret_cast<const f32x4 *>(area + ((wave ^ r) * UNITS + u) * 1024 + lane * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mine[u][i] = __builtin_fmaf(z[i], w, mine[u][i]);
+            }
+        }
+        if (whole) {
+            write_quarter(job.row0, job.t, cols, mine, 1.0f / sum);
+        } else {
             auto owner = [&](int y) -> int {             // the range that has position y of the sequence
                 const int cut = div_r * (div_q + 1);
                 return __builtin_amdgcn_readfirstlane(y < cut ? (int)((uint32_t)y / (uint32_t)(div_q + 1)) : div_r + (int)((uint32_t)(y - cut) / (uint32_t)div_q));
             };
-            w0 = owner(pos);
-            piece = wg - w0;
-            const int pieces = owner(pos + job.steps - 1) - w0 + 1;
+            const int w0 = owner(pos), pieces = owner(pos + job.steps - 1) - w0 + 1;
             if (cuts == 0) { cut_row0[0] = job.row0; cut_n[0] = job.n; cut_t[0] = job.t; cut_counter[0] = w0 * p.Hkv + kh; cut_pieces[0] = pieces; cut_w0[0] = w0; }
             else { cut_row0[1] = job.row0; cut_n[1] = job.n; cut_t[1] = job.t; cut_counter[1] = w0 * p.Hkv + kh; cut_pieces[1] = pieces; cut_w0[1] = w0; }
             ++cuts;
-        }
-        float *part = place_of(w0, piece);
-        const int cols = min(kCols, job.n * g - kCols * job.t);
-        for (int c0 = 0; c0 < cols; c0 += kMergeCols) {
-            if (c0 != 0) lds_barrier();                  // everybody is done with the columns before
+            float *part = place_of(w0, wg - w0);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int col = 16 * nb + l16;
-                if (col >= c0 && col < c0 + kMergeCols) x.put(nb, area[wave][col - c0], grp);
-            }
-            lds_barrier();
-            for (int v = tid; v < min(cols - c0, kMergeCols) * (D / 2); v += NT) {
-                const int cc = v / (D / 2), col = c0 + cc, d = 2 * (v - cc * (D / 2));
-                float ms = stat[0][0][col];
-#pragma unroll
-                for (int i = 1; i < NW; ++i) ms = fmaxf(ms, stat[i][0][col]);
-                float a = 0.f, b = 0.f, l = 0.f;
-#pragma unroll
-                for (int i = 0; i < NW; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(stat[i][0][col] - ms);
-                    const float2 z = *reinterpret_cast<const float2 *>(&area[i][cc][d]);
-                    a = __builtin_fmaf(z.x, w, a);
-                    b = __builtin_fmaf(z.y, w, b);
-                    l = __builtin_fmaf(stat[i][1][col], w, l);
-                }
-                if (whole) {
-                    write_pair(out_of(job.row0, kCols * job.t + col) + d, a, b, 1.0f / l);
-                } else {
-                    store_coherent2(part + col * D + d, a, b);
-                    if (d == 0) {
-                        store_coherent(part + kCols * D + col, ms);
-                        store_coherent(part + kCols * D + kCols + col, l);
-                    }
-                }
+            for (int u = 0; u < UNITS; ++u) store_coherent(reinterpret_cast<f32x4 *>(part) + (wave * UNITS + u) * 64 + lane, mine[u]);
+            if (grp == 0 && my_j == 0) {
+                store_coherent(part + kCols * D + my_col, top);
+                store_coherent(part + kCols * D + kCols + my_col, sum);
             }
         }
-        if (left == 0) break;
-        next_job(job, left, pos);
-        if (job.end == 0) break;
+        if (!more) break;
+        job = after;
+        pos = after_pos;
         lds_barrier();                                   // everybody is done with stat and area
+        load_q(job);
+        wait_vm<0>();
+        lds_barrier();
     }
     if (cuts == 0) return;
     coherent_stores_done();
@@ -415,75 +472,44 @@ __global__ __launch_bounds__(kWaves * 64, 2) void prefill_fp4_kernel(PrefillFp4P
     for (int k = 0; k < cuts; ++k) {
         const int pieces = k == 0 ? cut_pieces[0] : cut_pieces[1], first = k == 0 ? cut_w0[0] : cut_w0[1];
         if (__builtin_amdgcn_readfirstlane(arrived[k]) != pieces - 1) continue;
-        // all the others have been here: the counter goes back to zero, the parts are merged in their order
+        // all the others have been here: the counter goes back to zero, every wavefront merges its quarter of the parts, in their order, two at a time
         if (tid == 0) store_global(p.counters + (k == 0 ? cut_counter[0] : cut_counter[1]), 0);
         const int row0 = k == 0 ? cut_row0[0] : cut_row0[1], t = k == 0 ? cut_t[0] : cut_t[1], cols = min(kCols, (k == 0 ? cut_n[0] : cut_n[1]) * g - kCols * t);
-        float (*wts)[kCols] = reinterpret_cast<float (*)[kCols]>(smem);              // (the ring is empty)
-        float *met = &area[0][0][0];                                                 // [8][kCols] of m, [8][kCols] of the row sum
-        static_assert(kBatch * kCols * 4 <= (int)sizeof(smem) && NT == 8 * kCols, "eight threads to a column");
-        // the largest exponent and the sum under it: of every eighth part first
-        const int col = tid % kCols, sub = tid / kCols;
-        float mm = -INFINITY, l = 0.f;
-        for (int i0 = sub; i0 < pieces; i0 += 8 * 4) {
-            float mi[4], li[4];
+        float top = -INFINITY, sum = 0.f;
+        f32x4 o[UNITS];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float *src = place_of(first, min(i0 + 8 * i, pieces - 1)) + kCols * D + col;
-                mi[i] = load_coherent(src);
-                li[i] = load_coherent(src + kCols);
+        for (int u = 0; u < UNITS; ++u) o[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int AT_ONCE = 4;
+        for (int i0 = 0; i0 < pieces; i0 += AT_ONCE) {
+            float mi[AT_ONCE], li[AT_ONCE];
+            float2 z[AT_ONCE][UNITS][2];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                const float *part = place_of(first, min(i0 + i, pieces - 1));
+                mi[i] = load_coherent(part + kCols * D + 16 * my_nb + l16);
+                li[i] = load_coherent(part + kCols * D + kCols + 16 * my_nb + l16);
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    z[i][u][0] = load_coherent2(part + ((wave * UNITS + u) * 64 + lane) * 4);
+                    z[i][u][1] = load_coherent2(part + ((wave * UNITS + u) * 64 + lane) * 4 + 2);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i0 + 8 * i < pieces) {
-                    const float m_new = fmaxf(mm, mi[i]);
-                    l = __builtin_fmaf(li[i], __builtin_amdgcn_exp2f(mi[i] - m_new), l * __builtin_amdgcn_exp2f(mm - m_new));
-                    mm = m_new;
+            for (int i = 0; i < AT_ONCE; ++i)
+                if (i0 + i < pieces) {
+                    const float m_new = fmaxf(top, mi[i]), w_old = __builtin_amdgcn_exp2f(top - m_new), w = __builtin_amdgcn_exp2f(mi[i] - m_new);
+                    top = m_new;
+                    sum = __builtin_fmaf(li[i], w, sum * w_old);
+#pragma unroll
+                    for (int u = 0; u < UNITS; ++u) {
+                        o[u][0] = __builtin_fmaf(z[i][u][0].x, w, o[u][0] * w_old);
+                        o[u][1] = __builtin_fmaf(z[i][u][0].y, w, o[u][1] * w_old);
+                        o[u][2] = __builtin_fmaf(z[i][u][1].x, w, o[u][2] * w_old);
+                        o[u][3] = __builtin_fmaf(z[i][u][1].y, w, o[u][3] * w_old);
+                    }
                 }
         }
-        lds_barrier();                                   // everybody is done with area and the ring
-        met[sub * kCols + col] = mm;
-        met[(8 + sub) * kCols + col] = l;
-        lds_barrier();
-        float top = met[col], sum = 0.f;
-#pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, met[i * kCols + col]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(met[(8 + i) * kCols + col], __builtin_amdgcn_exp2f(met[i * kCols + col] - top), sum);
-        if (sub == 0) stat[0][0][col] = 1.0f / sum;
-        // ... then O, two neighbouring values of a column per thread and pass
-        constexpr int PASSES = kCols * (D / 2) / NT;
-        float a[PASSES], b[PASSES];
-#pragma unroll
-        for (int u = 0; u < PASSES; ++u) a[u] = b[u] = 0.f;
-        for (int b0 = 0; b0 < pieces; b0 += kBatch) {
-            const int n = min(kBatch, pieces - b0);
-            if (b0 != 0) lds_barrier();                  // everybody is done with the weights before
-            for (int i = sub; i < n; i += 8) wts[i][col] = __builtin_amdgcn_exp2f(load_coherent(place_of(first, b0 + i) + kCols * D + col) - top);
-            lds_barrier();
-            for (int i0 = 0; i0 < n; i0 += 4) {
-                float2 z[4][PASSES];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int u = 0; u < PASSES; ++u) z[i][u] = load_coherent2(place_of(first, b0 + min(i0 + i, n - 1)) + 2 * (tid + u * NT));
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i0 + i < n) {
-#pragma unroll
-                        for (int u = 0; u < PASSES; ++u) {
-                            const float w = wts[i0 + i][(tid + u * NT) / (D / 2)];
-                            a[u] = __builtin_fmaf(z[i][u].x, w, a[u]);
-                            b[u] = __builtin_fmaf(z[i][u].y, w, b[u]);
-                        }
-                    }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < PASSES; ++u) {
-            const int v = tid + u * NT, cc = v / (D / 2), d = 2 * (v - cc * (D / 2));
-            if (cc < cols) write_pair(out_of(row0, kCols * t + cc) + d, a[u], b[u], stat[0][0][cc]);
-        }
-        lds_barrier();
+        write_quarter(row0, t, cols, o, 1.0f / sum);
     }
 }
 
