@@ -1177,7 +1177,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
         // Over 4-bit codes, where contexts are long, stream mode also takes what tail mode would run on four fifths of the compute units or fewer (256 rows of 32 heads
         // over 8: behind 16000 tokens 98 us, with tails 191, behind 3000 42 and 55, without any 14.6 and 14.7) and chunks of short segments (512 rows of the same
         // heads in 7 segments behind 0 to 3000 tokens 55.8 and 64.9, 20 behind 0 to 6000 76 and 96; 20 without any 16.7 and 12.6).
-        if (fp4 && streams && !(p.tiles >= 2 && long_segs && jobs <= cus && 5 * jobs > 4 * (int64_t)cus))
+        if (fp4 && streams && p.S <= 64 && !(p.tiles >= 2 && long_segs && jobs <= cus && 5 * jobs > 4 * (int64_t)cus))
             G = std::min(255, (cus - code_append) / groups);
         else if (p.tiles >= 2 && jobs <= cus && (size_t)p.tiles * groups * 4 <= h->scratch_units)
             p.helpers = helpers;

@@ -1,0 +1,75 @@
+"""The host layer of the calls over 4-bit codes and of the norm and rotation without a GPU: what is refused launches nothing, launches fit the handle's memory, which
+kernel a call goes to on both sides of the rules (tests/host_fp4.cpp, with a recording HIP runtime)."""
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2401_11181_amd import tetri
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIP_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
+
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir(os.path.join(HIP_INCLUDE, "hip")),
+                                reason="needs g++ and the HIP headers")
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("host") / "host_fp4")
+    csrc = os.path.join(ROOT, "paper_2401_11181_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-static-libasan", "-static-libubsan", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-I", HIP_INCLUDE,
+                    "-I", os.path.join(ROOT, "include"), "-I", csrc, os.path.join(ROOT, "tests", "host_fp4.cpp")] +
+                   [os.path.join(csrc, name) for name in ("tetri_fp4_host.cpp", "tetri_rope_host.cpp", "tetri_host.cpp", "tetri_plan.cpp")] +
+                   ["-o", exe], check=True)
+    return exe
+
+
+@pytest.mark.parametrize("check", ["refusals", "memory", "counters"])
+def test_host_layer(driver, check):
+    res = subprocess.run([driver, check], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0 and check + ": ok" in res.stdout, res.stdout + res.stderr
+
+
+# heads, kv heads, head_dim, chunk, segments; 256 compute units
+PREFILL = [
+    # short segments, tiles filled to a sixth and less / more; too few tiles
+    ((40, 40, 128, 256, 32), "small"), ((40, 40, 128, 256, 16), "small"), ((40, 40, 128, 512, 20), "small"), ((40, 40, 128, 256, 8), "stream"), ((40, 40, 128, 1024, 32), "tiles"),
+    ((32, 8, 128, 256, 64), "small"), ((32, 8, 128, 256, 32), "stream"), ((8, 2, 128, 256, 64), "stream"),
+    # heads of 64: up to half the chip's tiles
+    ((6, 2, 64, 256, 1), "small"), ((6, 2, 64, 2048, 1), "small"), ((32, 8, 64, 512, 1), "small"), ((40, 40, 64, 512, 1), "tails"), ((32, 8, 64, 1024, 8), "stream"),
+    # long segments: tails where they fill the chip
+    ((40, 40, 128, 512, 1), "tails"), ((32, 8, 128, 512, 1), "stream"), ((32, 8, 128, 512, 7), "stream"), ((32, 8, 128, 2048, 1), "tiles"), ((8, 2, 128, 256, 1), "stream"),
+    # more than 64 segments have no stream
+    ((8, 2, 128, 256, 65), "tails"),
+]
+
+
+@pytest.mark.parametrize("shape,kernel", PREFILL, ids=str)
+def test_choice_of_the_prefill_kernel(driver, shape, kernel):
+    res = subprocess.run([driver, "kernels", *map(str, shape)], capture_output=True, text=True, timeout=60)
+    assert res.returncode == 0 and res.stdout.strip() == kernel, (shape, res.stdout + res.stderr)
+
+
+# heads, kv heads, head_dim, requests, longest context
+DECODE = [((8, 8, 128, 1, 8000), "16 parts 0 ranges"), ((40, 40, 128, 64, 2048), "1 parts 0 ranges"), ((32, 8, 128, 48, 8192), "0 parts 64 ranges"),
+          ((40, 40, 128, 4, 300), "1 parts 0 ranges"), ((40, 40, 128, 16, 8000), "0 parts 12 ranges"), ((40, 40, 128, 48, 1500), "1 parts 0 ranges")]
+
+
+@pytest.mark.parametrize("shape,cut", DECODE, ids=str)
+def test_cut_of_a_decode_iteration(driver, shape, cut):
+    res = subprocess.run([driver, "kernels", *map(str, shape), "0", "0"], capture_output=True, text=True, timeout=60)
+    assert res.returncode == 0 and res.stdout.strip() == cut, (shape, res.stdout + res.stderr)
+
+
+def test_rope_arguments():
+    """What the binding refuses by itself."""
+    for make in (lambda: tetri.Rope(np.zeros(65)), lambda: tetri.Rope(np.zeros(8), axis=[0] * 7), lambda: tetri.Rope(np.zeros(8), axis=[0] * 7 + [1]),
+                 lambda: tetri.Rope(np.zeros(8), axis=[-1] * 8), lambda: tetri.Rope(np.zeros(8), axis=[256] * 8, num_axes=3)):
+        with pytest.raises(ValueError):
+            make()
+    r = tetri.Rope([1.0, 2.0, 3.0, 4.0] * 2, axis=[0, 1] * 4, num_axes=2, adjacent=True)
+    assert (r.struct.num_pairs, r.struct.num_axes, r.struct.adjacent) == (8, 2, 1) and list(r.struct.axis[:8]) == [0, 1] * 4
