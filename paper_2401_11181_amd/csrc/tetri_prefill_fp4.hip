@@ -332,10 +332,11 @@ __global__ __launch_bounds__(kWaves * 64, 3) void prefill_fp4_kernel(PrefillFp4P
         // for the loads of the last step behind it
         for (int cs = job.begin + wave; cs < min(job.end, job.cached); cs += NW) {
             lds_reads_done();
-            codes.read_v(my + place_out, grp, l16);
             if (neg) codes.negate_k();
             f32x4 sc[NB][2];
             x.scores(codes, q_of, sc);
+            __builtin_amdgcn_sched_barrier(0);
+            codes.read_v(my + place_out, grp, l16);
             --many;
             turn(place_out);
             if (many > 0) {
