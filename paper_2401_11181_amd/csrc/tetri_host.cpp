@@ -979,9 +979,10 @@ static bool plan_small_tiles(const tetri_ctx *h, int32_t num_segs, bool append, 
 }
 // Whether a chunk goes there.  The other kernel's tiles are 128 columns (32 to 128 rows) and 64 or 128 keys: twice the rate on full tiles, but most of a tile is idle
 // behind a short segment.
-//  - Heads of 128: chunks of many short segments, whose tiles are filled to a sixth on average and are four fifths of the compute units or more.  (256 rows of 40 heads in
-//    32 segments without context 24 us, the other kernel 44, behind 0 to 4000 tokens 121 and 231; 256 rows of 32 heads over 8 in 64 segments 18.7 and
-//    19.5, 65 and 133; but in 32 segments, filled to a fifth, 16.1 and 12.2 without context, 44 and 67 with; one segment of 512 rows 44 and 19.5.)
+//  - Heads of 128: chunks of many short segments, whose tiles are filled to a quarter on average and are four fifths of the compute units or more.  (256 rows of 40 heads in
+//    32 segments without context 24 us, the other kernel 44, behind 0 to 4000 tokens 121 and 231; 256 rows of 32 heads over 8 in 32 segments 15.6 and
+//    15.9, 40.8 and 66.7; 512 of 40 in 12, filled to a quarter, 29.6 and 23.4, 77.7 and 110.5; but in 8, filled to a third, 30.4 and 23.4, 78.7 and 78.5; one
+//    segment of 512 rows of 32 heads over 8 44 and 19.5.)
 //  - Heads of 64, where everything of a wavefront is in registers: as long as a chunk has no more columns than half the chip's tiles.  (256 rows of 6 heads over 2
 //    behind 4000 tokens 22 and 36 us, without context 8.9 and 11.8; 2048 rows 44 and 88, 26 and 39; 8 short segments of 1024 rows 25 and 11, behind 0 to 4000 tokens
 //    36 and 46.)
@@ -992,7 +993,7 @@ static bool small_tiles_preferred(const tetri_ctx *h, int32_t num_segs)
     const int64_t groups = h->cfg.num_q_heads / hpw, full = h->cfg.chunk_size * groups / (32 * rb), cus = std::max(h->num_cus, 1);
     if (h->cfg.head_dim == 64) return 2 * full <= cus;
     const int64_t bound = groups * tile_bound(h->cfg.chunk_size, num_segs, 32 * rb);
-    return 5 * bound >= 4 * cus && 6 * full <= bound;
+    return 5 * bound >= 4 * cus && 4 * full <= bound;
 }
 
 static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, const void *k_new, const void *v_new,

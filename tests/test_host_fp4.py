@@ -36,9 +36,9 @@ def test_host_layer(driver, check):
 
 # heads, kv heads, head_dim, chunk, segments; 256 compute units
 PREFILL = [
-    # short segments, tiles filled to a sixth and less / more; too few tiles
-    ((40, 40, 128, 256, 32), "small"), ((40, 40, 128, 256, 16), "small"), ((40, 40, 128, 512, 20), "small"), ((40, 40, 128, 256, 8), "stream"), ((40, 40, 128, 1024, 32), "tiles"),
-    ((32, 8, 128, 256, 64), "small"), ((32, 8, 128, 256, 32), "stream"), ((8, 2, 128, 256, 64), "stream"),
+    # short segments, tiles filled to a quarter and less / more; too few tiles
+    ((40, 40, 128, 256, 32), "small"), ((40, 40, 128, 256, 8), "small"), ((40, 40, 128, 512, 12), "small"), ((40, 40, 128, 512, 8), "stream"), ((40, 40, 128, 1024, 20), "tiles"),
+    ((32, 8, 128, 256, 64), "small"), ((32, 8, 128, 256, 32), "small"), ((32, 8, 128, 512, 20), "stream"), ((8, 2, 128, 256, 64), "stream"),
     # heads of 64: up to half the chip's tiles
     ((6, 2, 64, 256, 1), "small"), ((6, 2, 64, 2048, 1), "small"), ((32, 8, 64, 512, 1), "small"), ((40, 40, 64, 512, 1), "tails"), ((32, 8, 64, 1024, 8), "stream"),
     # long segments: tails where they fill the chip
