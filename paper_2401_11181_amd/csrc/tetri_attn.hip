@@ -131,6 +131,10 @@ __device__ __forceinline__ void zero_padding_rows(const AttnParams &p, int grp, 
 // 19.4 us, cut 23.7; 128 rows in 6 segments without much, 40 heads: 14.6 and 19.3; but behind 500 cached tokens 8 heads over 2, 128 rows, 23.0 and
 // 18.5.)
 constexpr int kWholeStages = 4;
+// ... and a tile counts with this many more than it has (behind its own): its end, which is masked and of other rows, another tile's beginning and a result handed over
+// take a workgroup that has a border in its range that much longer.  (512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens 57.2 us without, 2 54.3,
+// 4 53.2, 6 56.1, 10 60.0; 1024 in 4 behind 0 to 4000 76.2, 60.1, 60.8, 64.9, 69.1; 512 of 8 over 2 in 6 39.3, 28.5, 27.5, 27.2, 28.6.)
+constexpr int kTileStages = 4;
 
 template <int D, int KS, int BITS>
 __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(AttnParams p)
@@ -194,7 +198,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
     // stages shared by Gp workgroups; the tile the next job is in: tile j of nt in its segment,
     // starting at position tile_lin
     int pos = 0, b1 = 0, W = 1, Gp = 1, j = 0, nt = 1, tile_lin = 0, tile_index = 0;
-    bool whole_tiles = false;                        // ... or, over 4-bit codes, one tile to a workgroup
+    [[maybe_unused]] bool whole_tiles = false;                        // ... or, over 4-bit codes, one tile to a workgroup
     // stream mode, one segment whose block-table row fits two registers per lane: the whole row is fetched together
     // with the segment lengths, so that the pages of the workgroup's first stage, wherever its range starts, do not
     // cost a second round trip to memory
@@ -316,6 +320,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
             X.piece = piece; X.npieces = n_tail != 0 ? 2 : 1; X.wf = 0;
         }
     };
+    constexpr int extra = BITS == 4 ? kTileStages : 0;
     if (G == 0) {
         make_piece(p, first_want, seg, first_t0, false, J);
     } else {
@@ -331,7 +336,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         const int n = b - a;
         const int ntl = (n + BM - 1) >> bm_shift;                  // 0 for lanes past the last segment
         const int csl = (ctx_len + STAGE - 1) / STAGE;
-        const int wk = ntl > 0 ? ntl * csl + new_stages_before<STAGE>(ntl - 1, bm_shift) + (n + STAGE - 1) / STAGE : 0;
+        const int wk = ntl > 0 ? ntl * (csl + extra) + new_stages_before<STAGE>(ntl - 1, bm_shift) + (n + STAGE - 1) / STAGE : 0;
         if (lane < S) seg_tab[lane] = make_int4(a, n, ctx_len, 0);  // every wavefront writes the same values
         int t_incl = ntl, w_incl = wk;
 #pragma unroll
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         // few stages, cutting them gains less than putting the pieces together costs.
         if constexpr (BITS == 4) {
             const int T = __builtin_amdgcn_readlane(t_incl, 63);
-            whole_tiles = T <= G && W < kWholeStages * T;
+            whole_tiles = T <= G && W < (kWholeStages + extra) * T;
             if (whole_tiles) Gp = T;
         }
         if (widx >= Gp) return;
@@ -357,7 +362,8 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         pos = __builtin_amdgcn_readfirstlane((int)((uint32_t)(widx * W) / (uint32_t)Gp));
         b1 = __builtin_amdgcn_readfirstlane((int)((uint32_t)((widx + 1) * W) / (uint32_t)Gp));
         unsigned long long owner = __builtin_amdgcn_ballot_w64(pos >= w_incl - wk && pos < w_incl);
-        if (BITS == 4 && whole_tiles) owner = __builtin_amdgcn_ballot_w64(widx >= t_incl - ntl && widx < t_incl);
+        if constexpr (BITS == 4)
+            if (whole_tiles) owner = __builtin_amdgcn_ballot_w64(widx >= t_incl - ntl && widx < t_incl);
         if (owner == 0) return;                      // cannot happen for well-formed metadata
         const int o = __builtin_ctzll(owner);
         seg.s = o;
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         seg.n_s = __builtin_amdgcn_readlane(n, o);
         seg.L = __builtin_amdgcn_readlane(ctx_len, o);
         nt = __builtin_amdgcn_readlane(ntl, o);
-        const int cs = __builtin_amdgcn_readlane(csl, o);
+        const int cs = __builtin_amdgcn_readlane(csl, o) + extra;
         page = __builtin_amdgcn_readlane(pg, o);
         page_hi = __builtin_amdgcn_readlane(pg_hi, o);
         const int seg_lin = __builtin_amdgcn_readlane(w_incl - wk, o);
@@ -380,9 +386,11 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
             j = j0 + cnt - 1;
             if (cnt < 64) break;
         }
-        if (BITS == 4 && whole_tiles) j = widx - __builtin_amdgcn_readlane(t_incl - ntl, o);
+        if constexpr (BITS == 4)
+            if (whole_tiles) j = widx - __builtin_amdgcn_readlane(t_incl - ntl, o);
         tile_lin = seg_lin + j * cs + new_stages_before<STAGE>(j, bm_shift);
-        if (BITS == 4 && whole_tiles) { pos = tile_lin; b1 = W; }
+        if constexpr (BITS == 4)
+            if (whole_tiles) { pos = tile_lin; b1 = W; }
         tile_index = __builtin_amdgcn_readlane(t_incl - ntl, o) + j;
     }
 
@@ -391,15 +399,16 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         X.grp = grp; X.kh = kh; X.seg_cu = seg.seg_cu; X.n_s = seg.n_s; X.t0 = j << bm_shift; X.tile_index = tile_index;
         X.src = make_src<D, KS>(pp, kh, seg, X.t0);
         const int n_all = X.src.n_ctx_tiles + (X.src.n_new + STAGE - 1) / STAGE;
-        const int tile_end = tile_lin + n_all;
+        const int stages_end = tile_lin + n_all, tile_end = stages_end + extra;
         X.it_begin = pos - tile_lin;
-        X.it_end = min(b1, tile_end) - tile_lin;
+        X.it_end = min(b1, stages_end) - tile_lin;
         X.wf = __builtin_amdgcn_readfirstlane((int)((uint32_t)((tile_lin + 1) * Gp - 1) / (uint32_t)W));
-        const int wl = __builtin_amdgcn_readfirstlane((int)((uint32_t)(tile_end * Gp - 1) / (uint32_t)W));
+        const int wl = __builtin_amdgcn_readfirstlane((int)((uint32_t)(stages_end * Gp - 1) / (uint32_t)W));
         X.npieces = wl - X.wf + 1;
         X.piece = widx - X.wf;
-        pos = tile_lin + X.it_end;
-        if (BITS == 4 && whole_tiles) { X.wf = widx; X.npieces = 1; X.piece = 0; b1 = pos; }
+        pos = BITS == 4 ? min(b1, tile_end) : tile_lin + X.it_end;
+        if constexpr (BITS == 4)
+            if (whole_tiles) { X.wf = widx; X.npieces = 1; X.piece = 0; b1 = pos; }
         if (pos == tile_end) {
             tile_lin = tile_end;
             ++tile_index;
@@ -417,6 +426,13 @@ __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(Att
         }
     };
     if (G != 0) stream_job(p, J);
+    if constexpr (BITS == 4) {
+        if (G != 0 && J.it_begin >= J.it_end) {      // the range began behind a tile's stages: the cursor is at the next one
+            if (pos >= b1) return;
+            stream_job(p, J);
+            pages_fetched = false;
+        }
+    }
     TETRI_MARK(9);
 
     // ---- the first job's first stage and its Q rows.  The wavefronts of key part 0 reach this point

@@ -1176,8 +1176,8 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
         const int64_t jobs = (int64_t)(p.tiles - 1 + helpers - 1) * groups;
         const bool long_segs = (int64_t)p.C >= 256 * (int64_t)p.S, streams = (key_parts == 2 || h->attn_variant == 1) && (int64_t)p.tiles * groups < 2 * (int64_t)cus;
         // Over 4-bit codes, where contexts are long, stream mode also takes what tail mode would run on four fifths of the compute units or fewer (256 rows of 32 heads
-        // over 8: behind 16000 tokens 98 us, with tails 191, behind 3000 42 and 55, without any 14.6 and 14.7) and chunks of short segments (512 rows of the same
-        // heads in 7 segments behind 0 to 3000 tokens 55.8 and 64.9, 20 behind 0 to 6000 76 and 96; 20 without any 16.7 and 12.6).
+        // over 8: behind 16000 tokens 98 us, with tails 191, behind 3000 36 and 55, without any 14.6 and 14.7) and chunks of short segments (512 rows of the same
+        // heads in 7 segments behind 0 to 3000 tokens 55 and 65, 20 behind 0 to 6000 68 and 96; 20 without any 16.7 and 12.6).
         if (fp4 && streams && p.S <= 64 && !(p.tiles >= 2 && long_segs && jobs <= cus && 5 * jobs > 4 * (int64_t)cus))
             G = std::min(255, (cus - code_append) / groups);
         else if (p.tiles >= 2 && jobs <= cus && (size_t)p.tiles * groups * 4 <= h->scratch_units)
@@ -1188,7 +1188,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
             G = std::min(255, (cus - (kv_pages_w ? 8 : 0)) / groups);
     }
     const int stage = 64 * key_parts;
-    const int64_t stage_bound = (int64_t)p.tiles * (((int64_t)p.max_blocks * 16 + p.C) / stage + 2);
+    const int64_t stage_bound = (int64_t)p.tiles * (((int64_t)p.max_blocks * 16 + p.C) / stage + (fp4 ? 2 + 4 : 2));
     if (G > 0 && (p.S > 64 || stage_bound * (G + 1) >= 0x7fffffffll || (size_t)groups * G * 4 > h->scratch_units || !counters_fit))
         G = 0;
     if (!counters_fit) p.helpers = 0;
