@@ -122,8 +122,8 @@ __global__ __launch_bounds__(kWaves * 64, NB == 1 ? 3 : 2) void decode_fp4_kerne
     }
     // the job after `j`, with `rest` steps of the range behind j: rest goes down by the new job's steps
     auto next_job = [&](Job &j, int &rest) {
-        ++j.b;
-        j.L = ctx_of(min(j.b, B - 1));
+        j.b = min(j.b + 1, B - 1);                       // (there is one, unless ctx_lens is written to while the launch runs)
+        j.L = ctx_of(j.b);
         j.begin = 0;
         j.end = min(j.steps(), rest);
         rest -= min(j.steps() + kRequestSteps, rest);

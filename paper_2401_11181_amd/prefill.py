@@ -114,6 +114,9 @@ class ChunkedPrefill:
     def qk_norm_rope(self, c, q, k, q_weight, k_weight, eps, rope, q_out, k_out, stream=None):
         """q and k of chunk c's rows (two-dimensional, their rows may lie in a fused projection), normed where there are weights and
         rotated by their positions, into q_out and k_out.  rope: a tetri.Rope."""
+        for x in (q, k):
+            if x.dim() != 2 or x.stride(1) != 1:
+                raise ValueError("q and k are rows whose elements follow each other, not %s with strides %s" % (tuple(x.shape), x.stride()))
         cu, ctx, _bt, S = self.meta[c]
         self.handle.tetri_qk_norm_rope(q, q.stride(0), k, k.stride(0), q_weight, k_weight, eps, rope, None, cu, ctx, S, self.C, q_out, k_out,
                                        stream)

@@ -6,8 +6,10 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2401_11181_amd import tetri
+from paper_2401_11181_amd.prefill import ChunkedPrefill
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HIP_INCLUDE = os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")
@@ -73,3 +75,11 @@ def test_rope_arguments():
             make()
     r = tetri.Rope([1.0, 2.0, 3.0, 4.0] * 2, axis=[0, 1] * 4, num_axes=2, adjacent=True)
     assert (r.struct.num_pairs, r.struct.num_axes, r.struct.adjacent) == (8, 2, 1) and list(r.struct.axis[:8]) == [0, 1] * 4
+
+
+def test_rows_for_the_rotation():
+    """A chunk's q and k have their rows' elements next to each other."""
+    good = torch.zeros((4, 8))
+    for q, k in ((good.T, good), (good, good[:, ::2]), (good.view(4, 2, 4), good), (good, good[0])):
+        with pytest.raises(ValueError):
+            ChunkedPrefill.qk_norm_rope(None, 0, q, k, None, None, 1e-6, None, None, None)
