@@ -1,5 +1,5 @@
-// Chunked-prefill attention over a paged cache of 4-bit codes for gfx950 where chunks give little work: tetri_attn.hip's kernel gives a row tile to a
-// workgroup, which then walks all keys, 128 at a time, behind barriers; here a tile is a quarter as large and any number of workgroups share its keys.
+// Chunked-prefill attention over a paged cache of 4-bit codes for gfx950 where segments are short, or heads 64 wide: tetri_attn.hip's kernel has tiles of 128
+// columns, whose keys a few workgroups walk 64 or 128 at a time, behind barriers; here a tile is a quarter as large and any number of workgroups share its keys.
 //
 //   * A tile is 32 columns of one kv head: neighbouring (row, query head of the kv head) pairs of a segment, rows first, so that codes become bf16
 //     once for all heads that share them.  A wavefront takes whole steps of 32 keys by itself (fp4_steps.h), from a ring in LDS, for all of the
