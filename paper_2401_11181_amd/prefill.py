@@ -65,6 +65,10 @@ class ChunkedPrefill:
         self._planned = list(self.meta)
         self._meta_version = None if self.meta_dev.is_inference() else self.meta_dev._version
 
+    def _is_planned(self, c):
+        """Whether the host's copies still say what chunk c's metadata on the device is."""
+        return self.meta[c] is self._planned[c] and (self._meta_version is None or self.meta_dev._version == self._meta_version)
+
     def chunk_segments(self, c):
         return [tuple(int(v) for v in s) for s in self.segs[self.offsets[c]:self.offsets[c + 1]]]
 
@@ -79,9 +83,8 @@ class ChunkedPrefill:
         return rows
 
     def _launch(self, c, q, k_new, v_new, kv_pages, scale, append, fp8, k_scale, v_scale, out, stream):
-        meta = self.meta[c]
-        cu, ctx, bt, S = meta
-        if meta is self._planned[c] and (self._meta_version is None or self.meta_dev._version == self._meta_version):
+        cu, ctx, bt, S = self.meta[c]
+        if self._is_planned(c):
             host_cu, host_ctx = self._host_meta[c]
             self.handle.tetri_chunk_prefill_planned(q, k_new, v_new, kv_pages, bt, cu, ctx, S, scale, append, fp8, k_scale, v_scale,
                                                     host_cu, host_ctx, out, stream)
@@ -113,10 +116,18 @@ class ChunkedPrefill:
 
     def qk_norm_rope(self, c, q, k, q_weight, k_weight, eps, rope, q_out, k_out, stream=None):
         """q and k of chunk c's rows (two-dimensional, their rows may lie in a fused projection), normed where there are weights and
-        rotated by their positions, into q_out and k_out.  rope: a tetri.Rope."""
+        rotated by their positions, into q_out and k_out.  rope: a tetri.Rope.  Padding rows are neither read nor written: tensors
+        that end with the chunk's last row will do (with metadata of one's own, which may have as many: the chunk size)."""
         for x in (q, k):
             if x.dim() != 2 or x.stride(1) != 1:
                 raise ValueError("q and k are rows whose elements follow each other, not %s with strides %s" % (tuple(x.shape), x.stride()))
+        rows = int(self._host_arrays[0][c][-1]) if self._is_planned(c) else self.C
+        for x, out, width in ((q, q_out, self.Hq * self.D), (k, k_out, self.Hkv * self.D)):
+            if x.shape[0] < rows or x.shape[1] < width:
+                raise ValueError("rows of q or k: %s, at least %s needed" % (tuple(x.shape), (rows, width)))
+            if isinstance(out, torch.Tensor) and (not out.is_contiguous() or out.numel() < rows * width):
+                raise ValueError("rows of q_out or k_out: %s with strides %s, contiguous and at least %s needed" %
+                                 (tuple(out.shape), out.stride(), (rows, width)))
         cu, ctx, _bt, S = self.meta[c]
         self.handle.tetri_qk_norm_rope(q, q.stride(0), k, k.stride(0), q_weight, k_weight, eps, rope, None, cu, ctx, S, self.C, q_out, k_out,
                                        stream)
@@ -136,7 +147,7 @@ class ChunkedPrefill:
 
     def _longest_ctx(self, c):
         # (an entry of `meta` that has been replaced may have any contexts that the block table can hold)
-        if self.meta[c] is self._planned[c] and (self._meta_version is None or self.meta_dev._version == self._meta_version):
+        if self._is_planned(c):
             return max(start for _, start, _ in self.chunk_segments(c))
         return self.max_blocks * 16
 
