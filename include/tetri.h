@@ -450,7 +450,9 @@ TETRI_API tetri_status tetri_chunk_prefill_attn_fp8(tetri_ctx *ctx, const void *
  *   for bit.
  * tetri_decode_attn_fp4, tetri_chunk_prefill_attn_fp4: tetri_decode_attn and tetri_chunk_prefill_attn over such a pool.  The new token's or the chunk's
  *   own k_new / v_new (bf16) enter unquantised; with append = 1 their codes are also written to their slots of the pool (then kv_pages_fp4 is
- *   in/out and block_table must cover them), with append = 0 the pool is only read.  Cached values become bf16 exactly (below 2^-133: 0).
+ *   in/out and block_table must cover them), with append = 0 the pool is only read.  Cached values become bf16, which is
+ *   exact for e up to 252 (the quantising calls write no larger one but 255), subnormal numbers included; under an e of 253 or 254, in imported
+ *   blocks, magnitudes of 2^128 and more become infinities.
  * Other arguments, errors, the limits and the scratch-memory rule as for the 16-bit calls.  tetri_kv_select and what belongs to it have no form for
  * such a pool, nor have the calls with host metadata.
  */

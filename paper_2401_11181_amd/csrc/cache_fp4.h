@@ -18,7 +18,8 @@ template <int D> constexpr uint32_t kFp4Codes = kPage * D / 2;
 // and 255 makes NaN of every code.
 __device__ __forceinline__ float fp4_scale(uint32_t exponent) { return __builtin_bit_cast(float, exponent << 23); }
 
-// 8 codes to 8 bf16 values; exact, since a code has two significant bits (below bf16's smallest normal number: as far as its subnormal ones reach).
+// 8 codes to 8 bf16 values; exact, since a code has two significant bits and the smallest value, 2^-128, is a subnormal bf16 number (under exponents of 253 and 254
+// magnitudes of 2^128 and more become infinities).
 __device__ __forceinline__ u32x4 fp4_to_bf16(uint32_t codes, float scale)
 {
     u32x4 r;
