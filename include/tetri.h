@@ -214,7 +214,8 @@ TETRI_API tetri_status tetri_kv_append(tetri_ctx *ctx, const void *k_new, const 
  * rows of q / k_new / v_new are never read.  Page slots at positions >= ctx_lens[s] are never
  * read.  Arithmetic: bf16 inputs, fp32 accumulation (bf16 MFMA), online softmax in fp32, the
  * softmax weights are rounded to bf16 before the PV product, output rounded to bf16 (nearest
- * even).  Results are deterministic run to run.
+ * even).  Results are deterministic run to run.  A weight of 0 is a factor like any other: an infinity or a NaN in a row of v_new may make
+ * NaN of its element also in rows of its segment in front of it (this holds for all chunk-prefill calls; not for k_new, nor for other segments).
  *   q, k_new, v_new, kv_pages, block_table, cu_chunk_q_lens, ctx_lens: device, in.
  *   out: device, out.  num_segs, scale: host scalars.
  */
