@@ -134,7 +134,7 @@ constexpr int kWholeStages = 4;
 // ... and a tile counts with this many more than it has (behind its own): its end, which is masked and of other rows, another tile's beginning and a result handed over
 // take a workgroup that has a border in its range that much longer.  (512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens 57.2 us without, 2 54.3,
 // 4 53.2, 6 56.1, 10 60.0; 1024 in 4 behind 0 to 4000 76.2, 60.1, 60.8, 64.9, 69.1; 512 of 8 over 2 in 6 39.3, 28.5, 27.5, 27.2, 28.6.)
-constexpr int kTileStages = 4;
+constexpr int kTileStages = kFp4TileStages;
 
 template <int D, int KS, int BITS>
 __global__ __launch_bounds__(Shape<KS>::WAVES * 64, 2) void attn_tile_kernel(AttnParams p)

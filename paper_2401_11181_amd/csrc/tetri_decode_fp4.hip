@@ -19,7 +19,7 @@ constexpr int kWaves = 4;         // wavefronts of a workgroup
 constexpr int kDepth = 2;         // steps a wavefront's ring holds: three workgroups fit a compute unit (with four steps, two: 64 requests of 2048 tokens 124.6 us, 119.6)
 // What a request costs a range of steps beside its steps, in steps: another page table, another Q, a merge.  A division that did not count it gave some ranges
 // five short requests and let all others wait for them (48 requests of 16 to 8192 tokens, 32 heads over 8: 33.0 us, with it 20.3).
-constexpr int kRequestSteps = 8;
+constexpr int kRequestSteps = kFp4RequestSteps;
 
 // A workgroup's partial result: g rows of D floats (unnormalised O), then g of m and g of the row sum.
 template <int D> __device__ __forceinline__ int part_floats(int g) { return g * D + ((2 * g + 3) & ~3); }

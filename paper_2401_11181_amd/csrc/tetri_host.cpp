@@ -368,8 +368,8 @@ static tetri_status decode_common(const char *fn, tetri_ctx *h, const void *q, c
     p.hkv_magic = p.Hkv <= 1 ? 0u : (uint32_t)((0x100000000ull + p.Hkv - 1) / p.Hkv);
     p.ranges = 0;
     p.min_steps = h->decode_ranges > 0 ? 1 : (fp4 ? 8 : 4);
-    // (9 steps more for each request: what the ranges over 4-bit codes count beside its steps)
-    const bool divisible = num_reqs <= kDecodeLookup && num_reqs * ((int64_t)cfg.max_blocks_per_seq * cfg.page_size / 32 + (fp4 ? 10 : 1)) <= 0x7fffffff;
+    // (a request's steps: at most one more than the half pages, rounded down; over 4-bit codes what a range counts beside them, and one to spare)
+    const bool divisible = num_reqs <= kDecodeLookup && num_reqs * ((int64_t)cfg.max_blocks_per_seq * cfg.page_size / 32 + (fp4 ? 2 + kFp4RequestSteps : 1)) <= 0x7fffffff;
     const int64_t most_bytes = pairs * steps * (fp4 ? 2 * 32 * (cfg.head_dim / 2 + cfg.head_dim / 32) : 32 * 2 * cfg.head_dim * (fp8 ? 1 : 2));
     int64_t parts = h->decode_parts;
     if (parts == 0) {
@@ -974,7 +974,7 @@ static bool plan_small_tiles(const tetri_ctx *h, int32_t num_segs, bool append, 
     p.min_steps = 8;
     // (positions of the sequence, columns times query heads and workgroups times kv heads are 32-bit numbers in the kernel)
     const int64_t columns = (int64_t)p.C * p.g, tiles = columns / kPrefillFp4Cols + num_segs;
-    return ranges >= 1 && tiles * ((int64_t)p.max_blocks / 2 + p.C / 32 + 8) <= 0x7fffffff && (columns + kPrefillFp4Cols) * p.g < 0xffffffffll &&
+    return ranges >= 1 && tiles * ((int64_t)p.max_blocks / 2 + p.C / 32 + 4 + kPrefillFp4TileSteps) <= 0x7fffffff && (columns + kPrefillFp4Cols) * p.g < 0xffffffffll &&
            ranges * p.Hkv * p.Hkv < 0xffffffffll;
 }
 // Whether a chunk goes there.  The other kernel's tiles are 128 columns (32 to 128 rows) and 64 or 128 keys: twice the rate on full tiles, but most of a tile is idle
@@ -1188,7 +1188,7 @@ static tetri_status attn_common(const char *fn, tetri_ctx *h, const void *q, con
             G = std::min(255, (cus - (kv_pages_w ? 8 : 0)) / groups);
     }
     const int stage = 64 * key_parts;
-    const int64_t stage_bound = (int64_t)p.tiles * (((int64_t)p.max_blocks * 16 + p.C) / stage + (fp4 ? 2 + 4 : 2));
+    const int64_t stage_bound = (int64_t)p.tiles * (((int64_t)p.max_blocks * 16 + p.C) / stage + 2 + (fp4 ? kFp4TileStages : 0));
     if (G > 0 && (p.S > 64 || stage_bound * (G + 1) >= 0x7fffffffll || (size_t)groups * G * 4 > h->scratch_units || !counters_fit))
         G = 0;
     if (!counters_fit) p.helpers = 0;

@@ -355,6 +355,12 @@ struct CompactParams {
     int32_t B, Hkv, max_blocks, keep, recent;
 };
 
+// What divisions over 4-bit codes count beside the steps or stages that there are, known to the kernels that divide and to the host that checks their
+// numbers: stages of a row tile (tetri_attn.hip), steps of a request (tetri_decode_fp4.hip), steps of a small tile (tetri_prefill_fp4.hip).
+constexpr int32_t kFp4TileStages = 4;
+constexpr int32_t kFp4RequestSteps = 8;
+constexpr int32_t kPrefillFp4TileSteps = 4;
+
 // Prefill over a pool of 4-bit codes in tiles of so many columns (tetri_prefill_fp4.hip).
 constexpr int32_t kPrefillFp4Cols = 32;
 struct PrefillFp4Params {

@@ -24,7 +24,7 @@ using namespace tetri_dev;
 constexpr int kWaves = 4;         // wavefronts of a workgroup
 constexpr int kDepth = 2;         // steps a wavefront's ring holds
 constexpr int kNB = 2, kCols = 16 * kNB;        // columns of a tile
-constexpr int kTileSteps = 4;     // what a tile costs a range beside its steps, in steps
+constexpr int kTileSteps = kPrefillFp4TileSteps;      // what a tile costs a range beside its steps, in steps
 
 // A workgroup's partial result: its accumulators as they lie in registers (a vector of 4 per product and lane), then m and the row sum of the columns.
 template <int D> constexpr int kPartFloats = kCols * (D + 2);
