@@ -103,8 +103,9 @@ template <int D> __device__ __forceinline__ void append_rows(const PrefillFp4Par
 }
 
 // Three workgroups to a compute unit.  What bounds it is the vector unit: a step of 32 keys and 32 columns is 32 matrix instructions (about 16 clocks each) beside some
-// 160 others, and at heads of 128 the registers of a third of a SIMD do not hold everything: Q is read from LDS at every step, and values of a tile that steps do not need go to
-// scratch memory.  (With two workgroups, Q in registers and three steps in a ring, nothing in scratch: 512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens
+// 160 others, and at heads of 128 the registers of a third of a SIMD do not hold everything: Q is read from LDS at every step, and 110 registers (416 bytes a lane) are
+// kept in scratch memory.  Steps of cached keys use none of it; a step of the chunk's own rows, whose K and V are held together, loads 13 words and stores
+// 4, and a tile puts some 64 away and fetches them around its steps.  (Heads of 64: no scratch memory.)  (With two workgroups, Q in registers and three steps in a ring, nothing in scratch: 512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens
 // 65.9 us, 61.8 so; 256 of 8 over 2 behind 8000 43.0 and 40.1; 128 of 40 behind 0 to 4000 38.2 and 31.0.  Tiles of 64 columns: 65.0, 74.6 and 36.  Loads two
 // steps ahead: 63.1, 40.8 and 31.0, they are there in time so.)
 template <int D>
