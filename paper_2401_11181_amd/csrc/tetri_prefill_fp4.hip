@@ -102,8 +102,9 @@ template <int D> __device__ __forceinline__ void append_rows(const PrefillFp4Par
     }
 }
 
-// Three workgroups to a compute unit.  What bounds it is the vector unit: a step of 32 keys and 32 columns is 32 matrix instructions (about 16 clocks each) beside some
-// 160 others, and at heads of 128 the registers of a third of a SIMD do not hold everything: Q is read from LDS at every step, and 110 registers (416 bytes a lane) are
+// Three workgroups to a compute unit.  A step of 32 keys and 32 columns is 32 matrix instructions (about 16 clocks each) beside some 160 others: inside the loop the vector
+// unit is what bounds it.  A launch is as much what stands around the loops: 256 rows of 32 heads over 8 in 32 segments behind 0 to 4000 tokens, 46.7 us, about 10 steps to a
+// wavefront, have the vector unit busy for 32 % of the time and the matrix cores for 13, and write 59 MB (scratch memory, parts) where rows and codes are 2.4.  At heads of 128 the registers of a third of a SIMD do not hold everything: Q is read from LDS at every step, and 110 registers (416 bytes a lane) are
 // kept in scratch memory.  Steps of cached keys use none of it; a step of the chunk's own rows, whose K and V are held together, loads 13 words and stores
 // 4, and a tile puts some 64 away and fetches them around its steps.  (Heads of 64: no scratch memory.)  (With two workgroups, Q in registers and three steps in a ring, nothing in scratch: 512 rows of 32 heads over 8 in 7 segments behind 0 to 3000 tokens
 // 65.9 us, 61.8 so; 256 of 8 over 2 behind 8000 43.0 and 40.1; 128 of 40 behind 0 to 4000 38.2 and 31.0.  Tiles of 64 columns: 65.0, 74.6 and 36.  Loads two
